@@ -502,6 +502,159 @@ cw_status cw_qkv_rope_append(const void* x, const void* w, const void* bias, con
                              int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t num_blocks,
                              void* stream);
 
+/* ========================================================================
+ * The 8-bit layer path. With a reused prefix only the suffix is prefilled
+ * (paper Sec. 1 and 2.1), and what can be reused is what the cache holds: in
+ * 8 bits it holds twice the prefix blocks (Sec. 3.4: the engine evicts when
+ * its memory is full). The calls below are a layer's way from hidden states to
+ * attention output in 8 bits, for prompts and for single tokens:
+ * cw_add_rms_norm_fp8, cw_fp8_linear, cw_rope_append_fp8, then
+ * cw_suffix_prefill_attn_fp8 or cw_decode_attn_fp8.
+ *
+ * 8-bit values are e4m3 (OCP: largest 448, NaN 0x7F / 0xFF, no infinity), one
+ * byte each, rounded to nearest even. Sums are fp32 (cw_fp8_linear says where not).
+ *
+ * The 8-bit cache:
+ *   k8, v8            e4m3 [num_blocks, Hkv, 16, D]    block rows are tokens
+ *   k_scale, v_scale  fp32 [num_blocks, Hkv]           a value is code * scale
+ * Scales must be positive and finite; cw_rope_append_fp8 writes powers of two.
+ * Prefix lengths need not be multiples of 16 in these calls. Pointers are
+ * 16-byte aligned except those of scales and int32 arrays. Device calls are
+ * asynchronous on `stream`, and on the device that it belongs to, which has
+ * to be the current one.
+ * ======================================================================== */
+
+/* ------------------------------------------------------------------------
+ * Device: residual addition, root-mean-square norm and 8-bit rows. For row t:
+ *   h = bf16(x[t] + residual[t])      (x[t] where residual is NULL)
+ *   y = h / sqrt(mean(h^2) + eps) * weight
+ *   scales[t][b] = max|y| / 448 over columns 128 b .. 128 b + 127,
+ *   out8 = e4m3(y / scale)
+ * (scale 1 and zeros where max|h * weight| of the columns is below 2^-100, or below
+ * 2^-68 in a row whose sum of squares is above fp32). A row of h with an infinity or
+ * a NaN has NaN codes and scales 1; columns whose weight is infinite or NaN have
+ * NaN codes, and the scale comes from the others.
+ *   x, residual    device bf16 [rows, hidden], rows x_stride / residual_stride
+ *                  elements apart
+ *   weight         device bf16 [hidden]
+ *   residual_out   device bf16 [rows, hidden] contiguous, or NULL: h. It may be
+ *                  x or residual itself (same address and contiguous).
+ *   out8           device e4m3 [rows, hidden]
+ *   scales         device fp32 [rows, ceil(hidden / 128)]
+ * CW_EINVAL: NULL pointer, rows < 0, eps outside [1e-20, 1], a stride below
+ * hidden or no multiple of 8, a misaligned pointer. CW_EUNSUPPORTED: hidden not
+ * a multiple of 16 in [16, 16384], more than 2^31 - 1 rows. CW_EHIP: launch. */
+cw_status cw_add_rms_norm_fp8(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                              const void* weight, float eps, int64_t rows, int32_t hidden, void* residual_out,
+                              void* out8, float* scales, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: product of 8-bit rows and 8-bit weights with a scale per block of 128:
+ *   out[t][n] = bf16(bias[n] + sum_b x_scale[t][b] w_scale[n / 128][b]
+ *                              sum_{k = 128 b ..} x8[t][k] w8[n][k])
+ * The blocks are added in fp32 in ascending order whatever the other rows of the
+ * call are: a row's results do not depend on the batch. Within a block the sum is
+ * the matrix instruction's: of 8 consecutive products it keeps 13 bits below the
+ * exponent of the largest one.
+ *   x8       device e4m3 [rows, hidden]        x_scale  fp32 [rows, ceil(hidden / 128)]
+ *   w8       device e4m3 [features, hidden]    w_scale  fp32 [ceil(features / 128), ceil(hidden / 128)]
+ *   bias     device bf16 [features], or NULL for none
+ *   out      device bf16 [rows, features]
+ * CW_EINVAL: NULL pointer, rows < 0, a misaligned pointer. CW_EUNSUPPORTED:
+ * hidden or features not a multiple of 16 in [16, 2^20], more than 2^22 rows.
+ * CW_EHIP: launch failure. */
+cw_status cw_fp8_linear(const void* x8, const float* x_scale, const void* w8, const float* w_scale,
+                        const void* bias, int64_t rows, int32_t features, int32_t hidden, void* out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: rotary embedding of the suffix rows' queries and keys and the append
+ * of keys and values to the 8-bit cache (paper Sec. 2.1: KV memory managed in
+ * fixed-size blocks). Suffix row i of request r is token P_r + i; rot() is that
+ * of cw_qkv_rope_append, on values of the bf16 inputs in fp32.
+ *   q_out[t][h] = bf16(rot(q[t][h]))
+ *   K rows rot(k[t][g]), V rows v[t][g]; per cache block that gets rows and KV
+ *   head, with amax their largest finite magnitude,
+ *     need  = 2^e, e the smallest in [-100, 120] with amax <= 448 * 2^e
+ *     scale = need where the call writes the block's slot 0, else
+ *             max(the block's scale, need): then the block's earlier rows are
+ *             rounded to the new scale (exact but for values below the
+ *             smallest normal code)
+ *     code  = e4m3(value / scale); infinite and NaN values are NaN codes
+ * Slots behind a request's last token and all other blocks keep their bytes. A
+ * table entry outside [0, num_blocks) drops its tokens. No two requests may
+ * write the same block.
+ *   q, k, v     device bf16 rows of Hq / Hkv heads of D values, q_stride /
+ *               k_stride / v_stride elements apart (slices of one projection)
+ *   q_out       device bf16 [total_s, Hq, D]; q and q_out both NULL: no queries
+ *   rope        device fp32 [rope_len, D / 2, 2] as cw_rope_table writes it;
+ *               NULL: keys are stored as they are (and q must be NULL)
+ *   cu_suffix, prefix_len   as for cw_kv_append. The launch depends on
+ *               cu_suffix alone: a captured call can be replayed with other
+ *               prefix lengths in prefix_len_dev (at most rope_len and
+ *               16 * bt_stride tokens with the suffix; beyond, tokens are
+ *               dropped or rotated by the last position, never a fault).
+ * CW_EINVAL: NULL pointer, batch < 1, num_kv_heads < 1, P_r < 0, cu not
+ * non-decreasing from 0, ceil(L_r / 16) > bt_stride, num_blocks < 1, a stride
+ * below the heads' columns or no multiple of 8, q without rope, rope_len below
+ * the longest prompt, a misaligned pointer. CW_EUNSUPPORTED: head_dim not
+ * 64/128, block_size != 16, more than 65536 KV heads, batch too large.
+ * CW_EHIP: launch failure. */
+cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, const float* rope, int32_t rope_len, void* q_out, void* k8, void* v8,
+                             float* k_scale, float* v_scale, const int32_t* block_table, int32_t bt_stride,
+                             const int32_t* cu_suffix_dev, const int32_t* prefix_len_dev,
+                             const int32_t* cu_suffix_host, const int32_t* prefix_len_host, int32_t batch,
+                             int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                             int32_t num_blocks, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: cw_suffix_prefill_attn over the 8-bit cache, which must already hold
+ * prefix and suffix. Keys and values are code * scale, exactly; q and out are
+ * bf16. Probabilities times their value's scale are rounded to bf16 for the
+ * product with the codes; softmax and sums are fp32.
+ *   plan_host / plan_dev   the unsplit plan of cw_suffix_prefill_plan
+ * A table entry outside [0, num_blocks) is read as zero keys and values, each
+ * with score 0. A NaN code of a visible key or value makes the outputs that see
+ * it NaN; codes behind a prompt's end are never used.
+ * Errors as cw_suffix_prefill_attn (P_r need not be a multiple of 16), plus
+ * CW_EINVAL for a misaligned pointer. */
+cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, const void* v8, const float* k_scale,
+                                     const float* v_scale, const int32_t* block_table, int32_t bt_stride,
+                                     const int32_t* cu_suffix_host, const int32_t* prefix_len_host, int32_t batch,
+                                     int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                     int32_t block_size, int32_t num_blocks, float softmax_scale,
+                                     const int32_t* plan_host, const int32_t* plan_dev, void* out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: attention of one query row per request over the 8-bit cache (the next
+ * token after a prefill). For request r, query head h (KV head g = h / (Hq / Hkv)):
+ *   s_j = softmax_scale * <q[r, h, :], K_r[j, g, :]>, j = 0 .. seq_lens[r] - 1
+ *   out[r, h, :] = sum_j softmax(s)_j V_r[j, g, :]     (zeros for length 0)
+ * Lengths are read from device memory alone, and the launch does not depend on
+ * them: a captured call can be replayed as sequences grow. A length above
+ * 16 * bt_stride counts as that, one below 0 as 0. Table entries outside the
+ * pool and NaN codes as for cw_suffix_prefill_attn_fp8.
+ *   q, out       device bf16 [batch, Hq, D]
+ *   seq_lens_dev device int32 [batch]
+ *   num_splits   1 .. 64 runs that each sequence is cut into, combined as by
+ *                cw_lse_merge (for few requests with long sequences)
+ *   workspace    device, 16-byte aligned, at least
+ *                cw_decode_attn_fp8_workspace_bytes(batch, Hq, D, num_splits)
+ *                bytes (0 for one split: NULL); overwritten. Calls that may run
+ *                at the same time need workspaces of their own.
+ * CW_EINVAL: NULL pointer, batch < 1, Hq % Hkv != 0, num_blocks or bt_stride < 1,
+ * softmax_scale not finite and positive, num_splits out of range, a missing or
+ * too small workspace, a misaligned pointer. CW_EUNSUPPORTED: head_dim not
+ * 64/128, block_size != 16, Hq / Hkv > 128, more than 65536 KV heads, batch too
+ * large. CW_EHIP: launch failure. */
+int64_t cw_decode_attn_fp8_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t head_dim,
+                                           int32_t num_splits);
+cw_status cw_decode_attn_fp8(const void* q, const void* k8, const void* v8, const float* k_scale,
+                             const float* v_scale, const int32_t* block_table, int32_t bt_stride,
+                             const int32_t* seq_lens_dev, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                             int32_t head_dim, int32_t block_size, int32_t num_blocks, float softmax_scale,
+                             int32_t num_splits, void* workspace, int64_t workspace_bytes, void* out, void* stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement aid (not a step of the path). A roofline of the attention kernel
  * prices it against the data-sheet bf16 peak; the rate this card sustains

@@ -14,6 +14,8 @@ Modules
   ordering   the knowledge tree by its definition, reusable prefix depth l(O, T),
              Algorithm 1, the exhaustive argmax over all orders (paper Sec. 3.3,
              Eq. 1) and the baseline orders (Sec. 4).
+  fp8        e4m3 values, the norm with 8-bit rows, the block-scaled product and the
+             append into an 8-bit cache.
   projection the suffix QKV projection with rotary position embedding (the
              per-layer work that feeds the cache append and attention).
 
@@ -22,6 +24,6 @@ The only blocking anywhere is the independent-row chunking in `attention`, which
 bounds memory and does not change any row's arithmetic.
 
 Parity status: every function here is pinned by tests/test_oracle_pins.py,
-tests/test_ordering.py and tests/test_projection.py (brute force, closed forms, a library routine, published test vectors, the
+tests/test_ordering.py, tests/test_projection.py and tests/test_fp8.py (brute force, closed forms, a library routine, published test vectors, the
 paper's worked examples). No function is "parity unpinned".
 """

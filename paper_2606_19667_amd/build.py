@@ -29,7 +29,8 @@ HIPCC = os.path.join(ROCM, "bin", "hipcc")
 ARCH = "gfx950"
 
 HOST_SOURCES = ["cw_host.cpp", "cw_tree.cpp", "cw_proj.cpp"]
-HIP_SOURCES = ["cw_kernels.hip", "cw_qkv.hip", "cw_probe.hip"]
+HIP_SOURCES = ["cw_kernels.hip", "cw_qkv.hip", "cw_probe.hip", "cw_fp8.hip", "cw_fp8_prefill.hip",
+               "cw_fp8_linear.hip"]
 
 HIP_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
@@ -45,8 +46,11 @@ HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra"]
 # Per-source extra flags. The attention kernel's step has uniform (wave-wide)
 # branches only; structurizing them makes the register allocator keep two
 # copies of the 64-register output accumulator across the branch arms, which
-# overflows the 256-register budget of two waves per SIMD.
-EXTRA_FLAGS = {"cw_kernels.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"]}
+# overflows the 256-register budget of two waves per SIMD. The norm and the
+# append of the 8-bit path tell NaN and infinite values apart.
+EXTRA_FLAGS = {"cw_kernels.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"],
+               "cw_fp8_prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"],
+               "cw_fp8.hip": ["-fhonor-nans"]}
 
 
 def _run(cmd):

@@ -36,7 +36,7 @@ cw_status ok() {
 }
 
 cw_status check_batch(const int32_t* cu, const int32_t* plen, int32_t batch, int32_t block_size,
-                      int32_t bt_stride, int64_t* total_rows) {
+                      int32_t bt_stride, int64_t* total_rows, bool any_prefix) {
   if (batch < 1) return fail(CW_EINVAL, "batch must be >= 1");
   if (!cu || !plen) return fail(CW_EINVAL, "cu_suffix_host and prefix_len_host are required");
   if (block_size < 1) return fail(CW_EINVAL, "block_size must be >= 1");
@@ -44,9 +44,9 @@ cw_status check_batch(const int32_t* cu, const int32_t* plen, int32_t batch, int
   if (cu[0] != 0) return fail(CW_EINVAL, "cu_suffix[0] must be 0");
   for (int32_t r = 0; r < batch; ++r) {
     if (cu[r + 1] < cu[r]) return fail(CW_EINVAL, "cu_suffix must be non-decreasing");
-    if (plen[r] < 0 || plen[r] % block_size != 0)
+    if (plen[r] < 0 || (!any_prefix && plen[r] % block_size != 0))
       return fail(CW_EINVAL, "prefix_len[" + std::to_string(r) + "] = " + std::to_string(plen[r]) +
-                                 " is not a non-negative multiple of the block size");
+                                 (any_prefix ? " is negative" : " is not a non-negative multiple of the block size"));
     const int64_t L = int64_t(plen[r]) + (cu[r + 1] - cu[r]);
     const int64_t nb = (L + block_size - 1) / block_size;
     if (nb > bt_stride)
@@ -54,6 +54,22 @@ cw_status check_batch(const int32_t* cu, const int32_t* plen, int32_t batch, int
                                  " blocks but bt_stride is " + std::to_string(bt_stride));
   }
   if (total_rows) *total_rows = cu[batch];
+  return CW_OK;
+}
+
+cw_status check_cache_fp8(const char* what, const void* k8, const void* v8, const float* k_scale,
+                          const float* v_scale, const int32_t* block_table, int32_t num_kv_heads,
+                          int32_t head_dim, int32_t block_size, int32_t num_blocks) {
+  const std::string w(what);
+  if (!k8 || !v8 || !k_scale || !v_scale || !block_table)
+    return fail(CW_EINVAL, w + ": a required pointer is NULL");
+  if (num_kv_heads < 1) return fail(CW_EINVAL, w + ": num_kv_heads must be >= 1");
+  if (num_blocks < 1) return fail(CW_EINVAL, w + ": num_blocks must be >= 1");
+  if (head_dim != 64 && head_dim != 128) return fail(CW_EUNSUPPORTED, w + ": head_dim must be 64 or 128");
+  if (block_size != kBlockSize) return fail(CW_EUNSUPPORTED, w + ": block_size must be 16");
+  if (num_kv_heads > kMaxKvHeads) return fail(CW_EUNSUPPORTED, w + ": more than 65536 KV heads");
+  if (((reinterpret_cast<uintptr_t>(k8) | reinterpret_cast<uintptr_t>(v8)) & 15) != 0)
+    return fail(CW_EINVAL, w + ": the caches must be 16-byte aligned");
   return CW_OK;
 }
 

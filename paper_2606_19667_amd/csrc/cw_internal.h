@@ -85,10 +85,17 @@ uint64_t append_fingerprint(const int32_t* cu_suffix_host, const int32_t* prefix
 
 // Validates the ragged batch description shared by the device entry points.
 // Checks cu[0] == 0, cu non-decreasing, P_r >= 0 and a multiple of
-// block_size, ceil(L_r / block_size) <= bt_stride; sets *total_rows.
+// block_size (any P_r >= 0 with any_prefix: the calls over the 8-bit cache),
+// ceil(L_r / block_size) <= bt_stride; sets *total_rows.
 cw_status check_batch(const int32_t* cu_suffix_host, const int32_t* prefix_len_host,
                       int32_t batch, int32_t block_size, int32_t bt_stride,
-                      int64_t* total_rows);
+                      int64_t* total_rows, bool any_prefix = false);
+
+// Checks shared by the calls over the 8-bit cache (`what`: the call's name):
+// pointers and their alignment, heads, head_dim, block size and pool size.
+cw_status check_cache_fp8(const char* what, const void* k8, const void* v8, const float* k_scale,
+                          const float* v_scale, const int32_t* block_table, int32_t num_kv_heads,
+                          int32_t head_dim, int32_t block_size, int32_t num_blocks);
 
 // Number of (request, kv head, row run) tiles of a batch, before padding.
 int64_t count_tiles(const int32_t* cu_suffix_host, int32_t batch, int32_t num_kv_heads,

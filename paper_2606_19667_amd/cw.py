@@ -98,6 +98,15 @@ def _load() -> ctypes.CDLL:
         "cw_rope_table": (_i32, [_i32, _i32, ctypes.c_double, ctypes.POINTER(ctypes.c_float)]),
         "cw_qkv_rope_append": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp,
                                       _pi32, _pi32, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
+        "cw_add_rms_norm_fp8": (_i32, [_vp, _i64, _vp, _i64, _vp, _f32, _i64, _i32, _vp, _vp, _vp, _vp]),
+        "cw_fp8_linear": (_i32, [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp]),
+        "cw_rope_append_fp8": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                      _i32, _vp, _vp, _pi32, _pi32, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
+        "cw_suffix_prefill_attn_fp8": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _pi32, _pi32, _i32, _i32, _i32,
+                                              _i32, _i32, _i32, _f32, _pi32, _vp, _vp, _vp]),
+        "cw_decode_attn_fp8_workspace_bytes": (_i64, [_i32, _i32, _i32, _i32]),
+        "cw_decode_attn_fp8": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
+                                      _f32, _i32, _vp, _i64, _vp, _vp]),
         "cw_probe_mfma_bf16_flops": (_i64, [_i32, _i32]),
         "cw_probe_mfma_bf16": (_i32, [_vp, _i64, _vp, _i32, _i32, _vp]),
     }
@@ -120,6 +129,8 @@ EXPORTED = ("cw_abi_version", "cw_last_error", "cw_block_hashes", "cw_pool_creat
             "cw_noalloc_scratch_bytes", "cw_suffix_prefill_attn_split_noalloc",
             "cw_tree_create", "cw_tree_destroy", "cw_tree_num_nodes", "cw_tree_insert",
             "cw_tree_mark_stale", "cw_tree_order", "cw_rope_table", "cw_qkv_rope_append",
+            "cw_add_rms_norm_fp8", "cw_fp8_linear", "cw_rope_append_fp8", "cw_suffix_prefill_attn_fp8",
+            "cw_decode_attn_fp8_workspace_bytes", "cw_decode_attn_fp8",
             "cw_probe_mfma_bf16_flops", "cw_probe_mfma_bf16")
 
 
@@ -711,6 +722,250 @@ def lse_merge(partial_o: torch.Tensor, partial_lse: torch.Tensor, out: torch.Ten
         raise ValueError(f"out must be [{rows}, {D}]")
     _check(_lib.cw_lse_merge(_dev(partial_o, torch.float32, "partial_o"), _dev(partial_lse, torch.float32, "partial_lse"),
                              parts, rows, D, _dev(out, torch.bfloat16, "out"), _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------- the 8-bit layer path
+FP8 = torch.float8_e4m3fn
+FP8_GROUP = 128    # columns of an 8-bit row (and rows of 8-bit weights) that share a scale
+
+
+def _rows(t: torch.Tensor, dtype, name: str, dim: int) -> tuple[int, int]:
+    """(address, elements from one row to the next) of a tensor whose rows are
+    contiguous and may lie apart (a slice of the columns of a larger one)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be in GPU memory")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != dim:
+        raise ValueError(f"{name} must have {dim} dimensions, got {t.dim()}")
+    width = 1
+    for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size > 1 and step != width:
+            raise ValueError(f"{name}: the elements of a row must be contiguous")
+        width *= size
+    if t.shape[0] > 1 and t.stride(0) < width:
+        raise ValueError(f"{name}: rows overlap")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else width)
+
+
+def _same_device(first: torch.Tensor, *others) -> None:
+    """The tensors of a call lie on one GPU, the current one (whose stream the
+    call takes): kernels would fault on another GPU's memory."""
+    if first.is_cuda and first.device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {first.device}, the current device is cuda:{torch.cuda.current_device()}")
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+
+
+class Fp8KvCache:
+    """An 8-bit paged KV cache: k, v float8_e4m3fn [num_blocks, Hkv, 16, D] and
+    k_scale, v_scale fp32 [num_blocks, Hkv]. A value is its code times the scale
+    of its (block, head); rope_append_fp8 writes powers of two."""
+
+    def __init__(self, num_blocks: int, num_kv_heads: int, head_dim: int, device="cuda"):
+        shape = (int(num_blocks), int(num_kv_heads), BLOCK_SIZE, int(head_dim))
+        self.k, self.v = (torch.empty(shape, dtype=FP8, device=device) for _ in range(2))
+        self.k_scale, self.v_scale = (torch.ones(shape[:2], dtype=torch.float32, device=device) for _ in range(2))
+
+    @classmethod
+    def of(cls, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor) -> "Fp8KvCache":
+        """The cache held in the given tensors (not copied)."""
+        self = cls.__new__(cls)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        if k.dim() != 4 or k.shape[2] != BLOCK_SIZE or v.shape != k.shape:
+            raise ValueError("k and v must both be [num_blocks, Hkv, 16, D]")
+        if k_scale.shape != k.shape[:2] or v_scale.shape != k.shape[:2]:
+            raise ValueError("k_scale and v_scale must be [num_blocks, Hkv]")
+        return self
+
+    @property
+    def num_blocks(self) -> int:
+        return int(self.k.shape[0])
+
+    def _args(self, num_kv_heads: int, head_dim: int):
+        if self.k.shape[1:] != (num_kv_heads, BLOCK_SIZE, head_dim):
+            raise ValueError(f"the cache holds {self.k.shape[1]} KV heads of {self.k.shape[3]}, "
+                             f"the call has {num_kv_heads} of {head_dim}")
+        return (_dev(self.k, FP8, "cache.k"), _dev(self.v, FP8, "cache.v"),
+                _dev(self.k_scale, torch.float32, "cache.k_scale"), _dev(self.v_scale, torch.float32, "cache.v_scale"))
+
+
+def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor | None = None,
+                     residual_out: torch.Tensor | None = None, out8: torch.Tensor | None = None,
+                     scales: torch.Tensor | None = None, stream=None):
+    """cw_add_rms_norm_fp8: h = x + residual in bf16, its root-mean-square norm
+    times weight, in 8 bits with a scale per 128 columns. x and residual are bf16
+    [rows, hidden] whose rows may lie apart. Returns (out8, scales, h); h is x
+    itself without a residual, else residual_out (which may be x or residual)."""
+    px, sx = _rows(x, torch.bfloat16, "x", 2)
+    T, H = x.shape
+    pr, sr = (None, 0) if residual is None else _rows(residual, torch.bfloat16, "residual", 2)
+    if residual is not None and residual.shape != x.shape:
+        raise ValueError(f"residual must be [{T}, {H}], got {tuple(residual.shape)}")
+    if weight.shape != (H,):
+        raise ValueError(f"weight must be [{H}], got {tuple(weight.shape)}")
+    if residual_out is None:
+        residual_out = x if residual is None else torch.empty((T, H), dtype=torch.bfloat16, device=x.device)
+        write = residual is not None
+    else:
+        write = True
+        if residual_out.shape != x.shape:
+            raise ValueError(f"residual_out must be [{T}, {H}]")
+    groups = -(-H // FP8_GROUP)
+    if out8 is None:
+        out8 = torch.empty((T, H), dtype=FP8, device=x.device)
+    elif out8.shape != x.shape:
+        raise ValueError(f"out8 must be [{T}, {H}]")
+    if scales is None:
+        scales = torch.empty((T, groups), dtype=torch.float32, device=x.device)
+    elif scales.shape != (T, groups):
+        raise ValueError(f"scales must be [{T}, {groups}]")
+    _same_device(x, residual, weight, residual_out, out8, scales)
+    _check(_lib.cw_add_rms_norm_fp8(
+        px, max(sx, H), pr, max(sr, H), _dev(weight, torch.bfloat16, "weight"), float(eps), T, H,
+        _dev(residual_out, torch.bfloat16, "residual_out") if write else None, _dev(out8, FP8, "out8"),
+        _dev(scales, torch.float32, "scales"), _stream(stream)))
+    return out8, scales, residual_out
+
+
+def fp8_linear(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w_scale: torch.Tensor,
+               bias: torch.Tensor | None = None, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """cw_fp8_linear: x8 [rows, hidden] times w8 [features, hidden] in 8 bits, with
+    x_scale [rows, ceil(hidden / 128)] and w_scale [ceil(features / 128),
+    ceil(hidden / 128)], plus bias [features] bf16; returns bf16 [rows, features]."""
+    if x8.dim() != 2 or w8.dim() != 2 or x8.shape[1] != w8.shape[1]:
+        raise ValueError(f"x8 must be [rows, hidden] and w8 [features, hidden], got {tuple(x8.shape)} and "
+                         f"{tuple(w8.shape)}")
+    (T, K), N = x8.shape, w8.shape[0]
+    groups = -(-K // FP8_GROUP)
+    if x_scale.shape != (T, groups):
+        raise ValueError(f"x_scale must be [{T}, {groups}], got {tuple(x_scale.shape)}")
+    if w_scale.shape != (-(-N // FP8_GROUP), groups):
+        raise ValueError(f"w_scale must be [{-(-N // FP8_GROUP)}, {groups}], got {tuple(w_scale.shape)}")
+    if bias is not None and bias.shape != (N,):
+        raise ValueError(f"bias must be [{N}], got {tuple(bias.shape)}")
+    if out is None:
+        out = torch.empty((T, N), dtype=torch.bfloat16, device=x8.device)
+    elif out.shape != (T, N):
+        raise ValueError(f"out must be [{T}, {N}]")
+    _same_device(x8, x_scale, w8, w_scale, bias, out)
+    _check(_lib.cw_fp8_linear(_dev(x8, FP8, "x8"), _dev(x_scale, torch.float32, "x_scale"), _dev(w8, FP8, "w8"),
+                              _dev(w_scale, torch.float32, "w_scale"),
+                              None if bias is None else _dev(bias, torch.bfloat16, "bias"), T, N, K,
+                              _dev(out, torch.bfloat16, "out"), _stream(stream)))
+    return out
+
+
+def rope_append_fp8(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp8KvCache,
+                    q: torch.Tensor | None = None, rope: torch.Tensor | None = None,
+                    q_out: torch.Tensor | None = None, stream=None) -> torch.Tensor | None:
+    """cw_rope_append_fp8: rotate the suffix rows' q [total_s, Hq, D] and k
+    [total_s, Hkv, D] with the table rope [n, D/2, 2] and write k and v to the
+    8-bit cache; the rows of q, k and v may lie apart (slices of one
+    projection). Returns q_out [total_s, Hq, D] bf16 (None without q). Without
+    rope (and q) keys are stored as they are. The prefix lengths of meta may be
+    any."""
+    if DEBUG_CHECK_COPIES:
+        meta.check_device_copies()
+    hq, hkv, D, T = meta.num_q_heads, meta.num_kv_heads, meta.head_dim, meta.total_rows
+    for name, t, h in (("q", q, hq), ("k", k, hkv), ("v", v, hkv)):
+        if t is not None and t.shape != (T, h, D):
+            raise ValueError(f"{name} must be [{T}, {h}, {D}], got {tuple(t.shape)}")
+    if rope is not None and (rope.dim() != 3 or rope.shape[1:] != (D // 2, 2)):
+        raise ValueError(f"rope must be [n, {D // 2}, 2], got {tuple(rope.shape)}")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    if q is not None and q_out is None:
+        q_out = torch.empty((T, hq, D), dtype=torch.bfloat16, device=q.device)
+    elif q_out is not None and q_out.shape != (T, hq, D):
+        raise ValueError(f"q_out must be [{T}, {hq}, {D}]")
+    pk, sk = _rows(k, torch.bfloat16, "k", 3)
+    pv, sv = _rows(v, torch.bfloat16, "v", 3)
+    pq, sq = (None, 0) if q is None else _rows(q, torch.bfloat16, "q", 3)
+    _same_device(cache.k, k, v, q, rope, q_out, cache.v, cache.k_scale, cache.v_scale, meta.bt, meta.cu, meta.plen)
+    ck, cv, cks, cvs = cache._args(hkv, D)
+    _check(_lib.cw_rope_append_fp8(
+        pq, max(sq, hq * D), pk, max(sk, hkv * D), pv, max(sv, hkv * D),
+        None if rope is None else _dev(rope, torch.float32, "rope"), 0 if rope is None else int(rope.shape[0]),
+        None if q_out is None else _dev(q_out, torch.bfloat16, "q_out"), ck, cv, cks, cvs,
+        _dev(meta.bt, torch.int32, "block_table"), meta.bt_stride, _dev(meta.cu, torch.int32, "cu_suffix"),
+        _dev(meta.plen, torch.int32, "prefix_len"), meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch,
+        hq, hkv, D, BLOCK_SIZE, cache.num_blocks, _stream(stream)))
+    return q_out
+
+
+def suffix_prefill_attn_fp8(meta: BatchMeta, q: torch.Tensor, cache: Fp8KvCache, softmax_scale: float,
+                            out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """cw_suffix_prefill_attn_fp8: attention of the suffix rows over the 8-bit
+    cache; returns out [total_s, Hq, D] bf16. The prefix lengths of meta may be any."""
+    if DEBUG_CHECK_COPIES:
+        meta.check_device_copies()
+    hq, hkv, D = meta.num_q_heads, meta.num_kv_heads, meta.head_dim
+    if q.shape != (meta.total_rows, hq, D):
+        raise ValueError(f"q must be [{meta.total_rows}, {hq}, {D}], got {tuple(q.shape)}")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    _same_device(cache.k, q, out, cache.v, cache.k_scale, cache.v_scale, meta.bt, meta.plan)
+    _check(_lib.cw_suffix_prefill_attn_fp8(
+        _dev(q, torch.bfloat16, "q"), *cache._args(hkv, D), _dev(meta.bt, torch.int32, "block_table"),
+        meta.bt_stride, meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE,
+        cache.num_blocks, float(softmax_scale), meta._hp(meta.plan_host), _dev(meta.plan, torch.int32, "plan"),
+        _dev(out, torch.bfloat16, "out"), _stream(stream)))
+    return out
+
+
+def decode_split_count(batch: int, num_q_heads: int, num_kv_heads: int, max_len: int) -> int:
+    """A split count for cw_decode_attn_fp8 with sequences of up to max_len tokens:
+    enough runs to fill the GPU, none of them below 256 tokens."""
+    tiles = max(1, int(batch) * int(num_kv_heads) * -(-int(num_q_heads) // (16 * int(num_kv_heads))))
+    return max(1, min(64, -(-768 // tiles), int(max_len) // 256))
+
+
+def decode_workspace_bytes(batch: int, num_q_heads: int, head_dim: int, num_splits: int) -> int:
+    n = int(_lib.cw_decode_attn_fp8_workspace_bytes(int(batch), int(num_q_heads), int(head_dim), int(num_splits)))
+    if n < 0:
+        _check(n)
+    return n
+
+
+def decode_attn_fp8(q: torch.Tensor, cache: Fp8KvCache, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                    softmax_scale: float, num_splits: int | None = None, workspace: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """cw_decode_attn_fp8: one query row per request, q [batch, Hq, D] bf16, over
+    the first seq_lens [batch] (int32, device) tokens of its row of block_table
+    [batch, stride] (int32, device); returns out [batch, Hq, D] bf16. `workspace`
+    (uint8, device) is allocated when not given; calls that may run at the same
+    time, captured ones among them, need one each."""
+    if q.dim() != 3:
+        raise ValueError(f"q must be [batch, Hq, D], got {tuple(q.shape)}")
+    B, hq, D = q.shape
+    hkv = int(cache.k.shape[1])
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"block_table must be [{B}, stride], got {tuple(block_table.shape)}")
+    if seq_lens.shape != (B,):
+        raise ValueError(f"seq_lens must be [{B}], got {tuple(seq_lens.shape)}")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    stride = int(block_table.shape[1])
+    if num_splits is None:
+        num_splits = decode_split_count(B, hq, hkv, stride * BLOCK_SIZE)
+    need = decode_workspace_bytes(B, hq, D, num_splits)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _same_device(cache.k, q, out, block_table, seq_lens, cache.v, cache.k_scale, cache.v_scale, workspace)
+    _check(_lib.cw_decode_attn_fp8(
+        _dev(q, torch.bfloat16, "q"), *cache._args(hkv, D), _dev(block_table, torch.int32, "block_table"), stride,
+        _dev(seq_lens, torch.int32, "seq_lens"), B, hq, hkv, D, BLOCK_SIZE, cache.num_blocks, float(softmax_scale),
+        int(num_splits), None if workspace is None else _dev(workspace, torch.uint8, "workspace"),
+        0 if workspace is None else workspace.numel(), _dev(out, torch.bfloat16, "out"), _stream(stream)))
     return out
 
 
