@@ -22,6 +22,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef const __attribute__((address_space(4))) int32_t cint32_t;
 
 constexpr int kBs = cw::kBlockSize;
 constexpr int kStep = cw::kKvTile;            // keys of a step (four blocks)
@@ -30,7 +31,7 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kBlocks = kStep / kBs;
 static_assert(kWaves * 32 == cw::kTileRows, "one 32-column MFMA block per wave");
 static_assert(kWaves == 2 * kBlocks, "a wave stages one block of one tensor");
-constexpr float kLazy = 8.0f;                 // the exponent base moves when a score exceeds it by 2^8
+constexpr float kMaxSum = 0x1p30f;            // a row's base moves when its sum exceeds this
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
@@ -67,9 +68,11 @@ template <int D>
 struct Geom {
   static constexpr int KP = 2 * D + 16;           // LDS bytes from one K row to the next (bf16, padded:
                                                   // the 16-byte reads of 8 rows lie on distinct banks)
-  static constexpr int VP = 2 * D + 32;           // the same of V (4 rows of a transposing read)
+  static constexpr int VP = 2 * D + 64;           // the same of V: the 4 rows x 64 bytes that half a wave
+                                                  // reads at once (transposing) lie on distinct banks
   static constexpr int KTILE = kStep * KP;
-  static constexpr int STAGE = KTILE + kStep * VP;
+  static constexpr int SCALES = KTILE + kStep * VP;   // k_scale, then v_scale of the step's blocks (fp32)
+  static constexpr int STAGE = SCALES + 2 * kBlocks * 4;
   static constexpr int PIECES = kBs * D / 1024;   // 16-byte pieces of a block that a lane stages
   static constexpr int KS = D / 16;               // MFMA k-steps over D
   static constexpr int DT = D / 32;               // 32-row output tiles over D
@@ -78,7 +81,8 @@ struct Geom {
 
 // Work as in the plan: an entry is (request, KV head g, a run of T suffix rows); 256 packed
 // rows of an entry are the G query heads of g over T = 256 / G positions, 32 a wave. Workgroup
-// w runs entries w, w + grid, ...; keys come in steps of 64.
+// w runs entries w, w + grid, ...; keys come in steps of 64, and the steps of all entries of a
+// queue form one stream.
 //  * A step's four blocks go through registers into LDS: wave w takes K (w even) or V (w odd)
 //    of block w / 2, converts the codes to bf16 (exact) and writes rows. So each code is
 //    converted once per workgroup, not once per wave. Rows past the prompt are zeros; a block
@@ -91,42 +95,140 @@ struct Geom {
 //    raw score, p v_scale = 2^(s (c k_scale) + (log2 v_scale - m)) is rounded to bf16 for the
 //    product, and the row's sum takes each block's rounded values divided by its v_scale. Q is
 //    not rounded again.
+//
+// The two waves of a SIMD alternate. A step j of a wave takes two intervals, each ended by a
+// workgroup barrier:
+//   softmax(j):   loads of step j + 3, 2^x packed to bf16, row sums (vector work)
+//   products(j):  O^T += V(j)^T P(j)^T, then S(j + 1) = K(j + 1) Q^T (matrix work), then the LDS
+//                 writes of step j + 2 (converted), which even out the two intervals
+// Waves 4-7 (group 1) run one interval behind waves 0-3. After an entry's last step S(j + 1) is the
+// next entry's first, so only the output and the change of queries come between two entries.
+//
+// Ring of three stages. Let softmax(s) of group 0 be interval 2 s, of group 1 2 s + 1; products(s) reads
+// V(s) and K(s + 1) in 2 s + 1 and 2 s + 2, the first V operands and the scales an interval earlier. Step x
+// is written in products(x - 2), 2 x - 3 and 2 x - 2, and first read (K) in 2 x - 1; the stage that it
+// replaces (step x - 3) was last read in 2 x - 4.
 template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void suffix_prefill_fp8_kernel(const PrefillArgs a) {
   using G = Geom<D>;
-  constexpr int KS = G::KS, DT = G::DT, P16 = G::PIECES;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * G::STAGE + kWaves * G::OUT];
-  // per stage: c_log2 * k_scale, log2(v_scale), 1 / v_scale of the step's blocks
-  __shared__ __attribute__((aligned(16))) float s_scale[2][3][kBlocks];
+  constexpr int KS = G::KS, DT = G::DT, P16 = G::PIECES, RING = 3;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[RING * G::STAGE + kWaves * G::OUT];
+  static_assert(RING * G::STAGE + kWaves * G::OUT <= 160 * 1024, "LDS of one CU");
 
-  if (uint32_t(a.plan[cw::kHdrFpLo]) != a.fp_lo || uint32_t(a.plan[cw::kHdrFpHi]) != a.fp_hi) return;
-  const int32_t* const ents = a.plan + cw::kPlanHeaderWords;
+  cint32_t* const plan = reinterpret_cast<cint32_t*>(reinterpret_cast<uintptr_t>(a.plan));
+  if (uint32_t(plan[cw::kHdrFpLo]) != a.fp_lo || uint32_t(plan[cw::kHdrFpHi]) != a.fp_hi) return;
+  const int grid = int(gridDim.x);
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool group1 = wave >= 4;
 
-  // ---- staging role
+  // ---- plan entries, word l % 16 in lane l; one that is not this batch's ends the queue. (Vector
+  // loads, here and below: a scalar load in flight would have to land before any LDS result.)
+  const int32_t* const ents = a.plan + cw::kPlanHeaderWords + (lane & 15);
+  auto fetch = [&](int e) __attribute__((always_inline)) -> int32_t {
+    return ents[int64_t(min(e, a.num_entries - 1)) * cw::kPlanEntryWords];
+  };
+  auto word = [](int32_t d, int i) __attribute__((always_inline)) -> int { return __builtin_amdgcn_readlane(d, i); };
+  auto valid = [&](int32_t d, int e) __attribute__((always_inline)) -> bool {
+    return e < a.num_entries && word(d, cw::kEntR) >= 0 &&
+           uint32_t(word(d, cw::kEntCheck)) == cw::entry_tag(a.fp_lo, a.fp_hi, uint32_t(e));
+  };
+  // ---- staging: this wave's tensor and block slot, and the cursor of its loads
   const bool is_v = (wave & 1) != 0;
   const int bs = wave >> 1;
   const uint8_t* const codes = is_v ? a.v8 : a.k8;
-  const float* const scales = is_v ? a.v_scale : a.k_scale;
   constexpr int LPR = D / 16;   // lanes a row
   const int skey = lane / LPR;  // row of the block, of piece 0
-  const int sdst = (is_v ? G::KTILE + bs * kBs * G::VP : bs * kBs * G::KP) + (lane % LPR) * 32;
   const int spitch = is_v ? G::VP : G::KP;
-
-  // ---- operand offsets
-  const int k_row = (l32 & ~12) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
-  const int k_off = k_row * G::KP + half * 16;
-  const int vj = lane & 15, vg = (lane >> 4) & 1;
-  const int v_off = G::KTILE + (8 * half + (vj >> 2)) * G::VP + (16 * vg + 4 * (vj & 3)) * 2;
-  auto rdk = [&](int base, int i) __attribute__((always_inline)) -> bf16x8 {   // k-step i / 2, keys 32 (i % 2) ..
-    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(lds + base + k_off + (i & 1) * 32 * G::KP +
-                                                                      (i >> 1) * 32));
+  const int sdst = (is_v ? G::KTILE + bs * kBs * G::VP : bs * kBs * G::KP) + skey * spitch + (lane % LPR) * 32;
+  int ce = blockIdx.x;          // index of the entry in c_next
+  int32_t c_next = fetch(ce);
+  int c_left = 0;               // steps of the cursor's entry not yet loaded
+  int c_keys = 0;               // keys of the prompt from the first of this wave's block on
+  uint32_t c_off = 0, c_max = 0;            // table word of the block, and of the prompt's last one (bytes)
+  const int32_t* c_row = a.bt;
+  const uint8_t* c_codes = codes;           // of the cursor's KV head, at this lane's piece
+  const float* c_scales = is_v ? a.v_scale : a.k_scale;
+  const uint32_t blk_bytes = uint32_t(a.hkv) * (kBs * D), blk_scales = uint32_t(a.hkv) * 4;
+  int32_t c_id = 0;             // the table word, loaded a step ahead (the same in every lane)
+  auto cursor_id = [&]() __attribute__((always_inline)) {
+    uint32_t off = min(c_off, c_max);
+    asm volatile("" : "+v"(off));           // (a vector load)
+    c_id = *reinterpret_cast<const int32_t*>(reinterpret_cast<const uint8_t*>(c_row) + off);
   };
-  auto rdv = [&](int base, int kk, int t) __attribute__((always_inline)) -> bf16x8 {   // block kk, columns 32 t ..
+  // The next entry of the queue. Past the last one the cursor stays in its last entry, behind the
+  // prompt's end: what it loads is staged as zeros.
+  auto cursor_take = [&]() __attribute__((always_inline)) {
+    c_left = INT32_MAX;
+    c_keys = 0;
+    if (!valid(c_next, ce)) return;
+    const int kbeg = word(c_next, cw::kEntKbeg), L = word(c_next, cw::kEntL), g = word(c_next, cw::kEntG);
+    c_left = word(c_next, cw::kEntKend) - kbeg;
+    c_keys = L - (kbeg * kBlocks + bs) * kBs;
+    c_off = uint32_t(kbeg * kBlocks + bs) * 4;
+    c_max = uint32_t((L + kBs - 1) / kBs - 1) * 4;
+    c_row = a.bt + int64_t(word(c_next, cw::kEntR)) * a.bt_stride;
+    c_codes = codes + int64_t(g) * (kBs * D);
+    c_scales = (is_v ? a.v_scale : a.k_scale) + g;
+    ce += grid;
+    c_next = fetch(ce);
+  };
+  u32x4 raw[P16];
+  float raw_scale = 1.f;
+  int raw_keys = 0;   // rows of the loaded block inside the prompt; 0 or less: none
+  auto load = [&]() __attribute__((always_inline)) {
+    // (a block outside the pool loads block 0 and is staged as zeros)
+    const bool ok = uint32_t(c_id) < uint32_t(a.num_blocks);
+    const uint32_t id = ok ? c_id : 0;
+    raw_keys = ok ? c_keys : 0;
+    const uint8_t* src = c_codes + (uint64_t(id) * blk_bytes + uint32_t(lane * 16));
+#pragma unroll
+    for (int i = 0; i < P16; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + 1024 * i);
+    raw_scale = *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(c_scales) + uint64_t(id) * blk_scales);
+    c_keys -= kStep;
+    c_off += 4 * kBlocks;
+    if (__builtin_expect(--c_left == 0, 0)) cursor_take();
+    cursor_id();
+  };
+  auto stage = [&](int at_stage) __attribute__((always_inline)) {
+    uint8_t* const dst = lds + at_stage + sdst;
+    const bool part = __builtin_amdgcn_ballot_w64(raw_keys < kBs) != 0;
+#pragma unroll
+    for (int i = 0; i < P16; ++i) {
+      u32x4 x = raw[i];
+      if (__builtin_expect(part, 0)) {
+        if (i * (64 / LPR) + skey >= raw_keys) x = u32x4{0, 0, 0, 0};
+      }
+      const u32x2 a0 = widen_fp8x4(x[0]), a1 = widen_fp8x4(x[1]), a2 = widen_fp8x4(x[2]), a3 = widen_fp8x4(x[3]);
+      u32x4* at = reinterpret_cast<u32x4*>(dst + i * (64 / LPR) * spitch);
+      at[0] = u32x4{a0[0], a0[1], a1[0], a1[1]};
+      at[1] = u32x4{a2[0], a2[1], a3[0], a3[1]};
+    }
+    if (lane == 0)
+      *reinterpret_cast<float*>(lds + at_stage + G::SCALES + (is_v * kBlocks + bs) * 4) = raw_keys > 0 ? raw_scale : 1.f;
+  };
+  auto barrier = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // ---- operands
+  int k_off = ((l32 & ~12) | ((l32 & 4) << 1) | ((l32 & 8) >> 1)) * G::KP + half * 16;
+  const int vj = lane & 15, vg = (lane >> 4) & 1;
+  int v_off = G::KTILE + (8 * half + (vj >> 2)) * G::VP + (16 * vg + 4 * (vj & 3)) * 2;
+  // (hidden bases: else the compiler keeps a register per offset instead of an immediate)
+  asm volatile("" : "+v"(k_off));
+  asm volatile("" : "+v"(v_off));
+  auto rdk = [&](int kb, int i) __attribute__((always_inline)) -> bf16x8 {   // k-step i / 2, keys 32 (i % 2) ..
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(lds + kb + (i & 1) * 32 * G::KP + (i >> 1) * 32));
+  };
+  auto rdv = [&](int vb, int i) __attribute__((always_inline)) -> bf16x8 {   // block i / DT, columns 32 (i % DT) ..
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    auto* lp = (__attribute__((address_space(3))) uint8_t*)lds + base + v_off + kk * kBs * G::VP + t * 64;
+    auto* lp = (__attribute__((address_space(3))) uint8_t*)lds + vb + (i / DT) * kBs * G::VP + (i % DT) * 64;
     const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lp));
     const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lp + 4 * G::VP)));
     return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
@@ -134,149 +236,172 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
 
   const int m_col = wave * 32 + l32;   // this lane's query column: head hh of the group, position pos
   const int hh = m_col / a.per_tile, pos = m_col - hh * a.per_tile;
-
-  for (int e = blockIdx.x; e < a.num_entries; e += gridDim.x) {
-    const int32_t* const d = ents + int64_t(e) * cw::kPlanEntryWords;
-    const int r = d[cw::kEntR];
-    if (r < 0 || uint32_t(d[cw::kEntCheck]) != cw::entry_tag(a.fp_lo, a.fp_hi, uint32_t(e))) return;
-    const int g = d[cw::kEntG], row0 = d[cw::kEntRow0], nvalid = d[cw::kEntNvalid], P = d[cw::kEntP],
-              L = d[cw::kEntL], kbeg = d[cw::kEntKbeg], nsteps = d[cw::kEntKend] - kbeg, n_full = d[cw::kEntNfull],
-              qrow0 = d[cw::kEntQrow];
-    const int32_t* const bt = a.bt + int64_t(r) * a.bt_stride;
-    const int last = (L + kBs - 1) / kBs - 1;
-
-    u32x4 raw[P16];
-    float scale = 1.f;
-    int keys = 0;   // rows of the staged block inside the prompt
-    auto load = [&](int j) __attribute__((always_inline)) {
-      const int lb = (kbeg + j) * kBlocks + bs;
-      const int id = bt[min(lb, last)];
-      const bool ok = lb <= last && id >= 0 && id < a.num_blocks;
-      const uint8_t* src = codes + (int64_t(ok ? id : 0) * a.hkv + g) * (kBs * D) + lane * 16;
-      keys = ok ? L - lb * kBs : 0;
-      scale = ok ? scales[int64_t(id) * a.hkv + g] : 1.f;
+  auto has_row = [&](int32_t x) __attribute__((always_inline)) -> bool {
+    return hh < a.group && pos < word(x, cw::kEntNvalid);
+  };
+  bf16x8 qf[KS];
+  // The queries of an entry. A lane without a row takes the entry's first: its column is not stored.
+  auto load_q = [&](int32_t x) __attribute__((always_inline)) {
+    const bool ok = has_row(x);
+    const int64_t row = int64_t(word(x, cw::kEntQrow)) + (ok ? pos : 0);
+    const int head = word(x, cw::kEntG) * a.group + (ok ? hh : 0);
+    const u32x4* src = reinterpret_cast<const u32x4*>(a.q + (row * a.hq + head) * D) + half;
 #pragma unroll
-      for (int i = 0; i < P16; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + 1024 * i);
-    };
-    auto stage = [&](int slot) __attribute__((always_inline)) {
-      uint8_t* const dst = lds + slot * G::STAGE + sdst;
-#pragma unroll
-      for (int i = 0; i < P16; ++i) {
-        const int key = i * (64 / LPR) + skey;
-        u32x4 x = raw[i];
-        if (key >= keys) x = u32x4{0, 0, 0, 0};
-        const u32x2 a0 = widen_fp8x4(x[0]), a1 = widen_fp8x4(x[1]), a2 = widen_fp8x4(x[2]), a3 = widen_fp8x4(x[3]);
-        u32x4* at = reinterpret_cast<u32x4*>(dst + key * spitch);
-        at[0] = u32x4{a0[0], a0[1], a1[0], a1[1]};
-        at[1] = u32x4{a2[0], a2[1], a3[0], a3[1]};
-      }
-      if (lane == 0) {
-        if (is_v) {
-          s_scale[slot][1][bs] = __log2f(scale);
-          s_scale[slot][2][bs] = 1.f / scale;
-        } else {
-          s_scale[slot][0][bs] = a.c_log2 * scale;
-        }
-      }
-    };
+    for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, src[2 * s]);
+  };
 
-    const bool row_ok = hh < a.group && pos < nvalid;
-    bf16x8 qf[KS];
-    {
-      const int64_t row = int64_t(qrow0) + (row_ok ? pos : 0);
-      const u32x4* src = reinterpret_cast<const u32x4*>(
-                             a.q + (row * a.hq + g * a.group + (row_ok ? hh : 0)) * D) + half;
+  int e_cur = blockIdx.x;
+  int32_t cur = fetch(e_cur), next = fetch(e_cur + grid);
+  if (!valid(cur, e_cur)) return;   // (the same for every wave)
+  cursor_take();
+  cursor_id();
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        u32x4 x = src[2 * s];
-        if (!row_ok) x = u32x4{0, 0, 0, 0};
-        qf[s] = __builtin_bit_cast(bf16x8, x);
-      }
+  for (int i = 0; i < 2; ++i) {
+    load();
+    stage(i * G::STAGE);
+  }
+  load_q(cur);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  barrier();
+
+  f32x16 sc[2];      // scores of the step whose softmax comes next
+  f32x16 oacc[DT];
+  uint32_t w[16];    // packed probabilities times their value's scale
+  float m = 0.f, l = 0.f;
+#pragma unroll
+  for (int t = 0; t < DT; ++t) oacc[t] = f32x16{};
+  const bf16x2 ones{(__bf16)1.0f, (__bf16)1.0f};
+
+  constexpr int RA = 6;   // operands in flight ahead of their MFMA
+  constexpr int NPV = kBlocks * DT, NQK = 2 * KS, N = NPV + NQK;
+  bf16x8 op[RA];
+  int st0 = 0, st1 = G::STAGE, st2 = 2 * G::STAGE;   // LDS places of the current step and the two after it
+  float kc[kBlocks], vlog[kBlocks], vinv[kBlocks];   // the current step's c k_scale, log2(v_scale), 1 / v_scale
+  f32x4 k_sc, v_sc;   // its scales, read at the end of the interval before
+  auto read_scales = [&]() __attribute__((always_inline)) {
+    k_sc = *reinterpret_cast<const f32x4*>(lds + st0 + G::SCALES);
+    v_sc = *reinterpret_cast<const f32x4*>(lds + st0 + G::SCALES + 4 * kBlocks);
+  };
+  read_scales();
+  auto row_max = [&]() __attribute__((always_inline)) -> float {   // of the current step's scaled scores
+    asm volatile("" : "+v"(sc[0]), "+v"(sc[1]));   // (else it is computed in every step, ahead of its branches)
+    float mx = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      float y = sc[b >> 1][(b & 1) * 8];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) y = fmaxf(y, sc[b >> 1][(b & 1) * 8 + i]);
+      mx = fmaxf(mx, y * kc[b]);
     }
-    const int qpos = P + row0 + pos;   // keys 0 .. qpos are visible
+    return max_pair32(mx);
+  };
+  if (group1) barrier();   // group 1 runs one interval behind
+#pragma unroll
+  for (int i = 0; i < NQK; ++i)
+    sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rdk(k_off, i), qf[i >> 1], i < 2 ? f32x16{} : sc[i & 1], 0, 0, 0);
+  barrier();
 
-    f32x16 oacc[DT];
-#pragma unroll
-    for (int t = 0; t < DT; ++t) oacc[t] = f32x16{};
-    float m = 0.f, l = 0.f;
-    load(0);
-    __syncthreads();   // the entry before is done with the stages
-    stage(0);
-    if (nsteps > 1) load(1);
-    __syncthreads();
+  for (;;) {
+    const int kbeg = word(cur, cw::kEntKbeg), nsteps = word(cur, cw::kEntKend) - kbeg;
+    const int n_full = word(cur, cw::kEntNfull), nvalid = word(cur, cw::kEntNvalid);
+    const int g = word(cur, cw::kEntG), qrow0 = word(cur, cw::kEntQrow);
+    const int qpos = word(cur, cw::kEntP) + word(cur, cw::kEntRow0) + pos;   // keys 0 .. qpos are visible
+    const bool more = valid(next, e_cur + grid);
     for (int j = 0; j < nsteps; ++j) {
-      if (j + 1 < nsteps) stage((j + 1) & 1);
-      if (j + 2 < nsteps) load(j + 2);
-      const int base = (j & 1) * G::STAGE;
-      f32x16 sc[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-      for (int i = 0; i < 2 * KS; ++i)
-        sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rdk(base, i), qf[i >> 1], sc[i & 1], 0, 0, 0);
-      float kc[kBlocks], vlog[kBlocks], vinv[kBlocks];
+      // ---- softmax interval
+      load();
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
-        kc[b] = s_scale[j & 1][0][b];
-        vlog[b] = s_scale[j & 1][1][b];
-        vinv[b] = s_scale[j & 1][2][b];
+        kc[b] = a.c_log2 * k_sc[b];
+        vlog[b] = __builtin_amdgcn_logf(v_sc[b]);
+        vinv[b] = __builtin_amdgcn_rcpf(v_sc[b]);
       }
-      if (j >= n_full) {
+      if (__builtin_expect(j == nsteps - 1, 0)) load_q(more ? next : cur);   // (first used after the PV products)
+      __builtin_amdgcn_sched_barrier(0);
+      if (__builtin_expect(j >= n_full, 0)) {
         const int lim = qpos - (kbeg + j) * kStep - half * 8;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          for (int i = 0; i < 16; ++i) {   // (pinned: else 32 compare results stay live in scalar registers)
             if (h * 32 + (i >> 3) * 16 + (i & 7) > lim) sc[h][i] = -INFINITY;
             asm volatile("" : "+v"(sc[h][i]));
           }
       }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        float x = sc[b >> 1][(b & 1) * 8];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) x = fmaxf(x, sc[b >> 1][(b & 1) * 8 + i]);
-        mx = fmaxf(mx, x * kc[b]);
-      }
-      mx = max_pair32(mx);
-      if (j == 0) {
+      // An entry's base is the exact row maximum of its first step, and moves only when the row's sum
+      // passes 2^30: bf16 and fp32 have the range for it, so later steps need no maximum (27 fewer
+      // vector instructions of 180 in the interval that bounds the kernel).
+      if (__builtin_expect(j == 0, 0)) {
+        const float mx = row_max();
         m = mx == -INFINITY ? 0.f : mx;
-      } else if (__builtin_amdgcn_ballot_w64(mx > m + kLazy) != 0) {
-        const float to = mx > m + kLazy ? mx : m;
+      }
+      float l_new;
+      for (;;) {
+        l_new = l;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+          const float add = vlog[b] - m;
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int at = (b & 1) * 8 + 2 * i;
+            w[4 * b + i] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(sc[b >> 1][at], kc[b], add)),
+                                       __builtin_amdgcn_exp2f(fmaf(sc[b >> 1][at + 1], kc[b], add)));
+            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[4 * b + i]), ones, sum, false);
+          }
+          l_new = fmaf(sum, vinv[b], l_new);
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(l_new > kMaxSum) == 0, 1)) break;
+        // (a second pass at most brings every row of the step to its own maximum: with l at 2^30
+        // or below and probabilities up to 1 the sum is in range again, so the loop ends)
+        const float before = max_pair32(l), top = max_pair32(l_new);   // (both halves hold the same row)
+        const float to = top > kMaxSum ? fmaxf(row_max(), before > 1.f ? m + __builtin_amdgcn_logf(before) : m) : m;
+        if (__builtin_amdgcn_ballot_w64(to != m) == 0) break;   // (nothing to move: values that are no numbers)
         const float alpha = __builtin_amdgcn_exp2f(m - to);
-        m = to;
         l *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) oacc[t] *= alpha;
+        m = to;
       }
-      uint32_t w[16];
-      const bf16x2 ones{(__bf16)1.0f, (__bf16)1.0f};
+      l = l_new;
+      const int vb = v_off + st0, kb = k_off + st1;
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        const float add = vlog[b] - m;
-        float sum = 0.f;
+      for (int i = 0; i < RA; ++i) op[i] = rdv(vb, i);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      barrier();
+
+      // ---- product interval: MFMA and operand read alternate, fenced so that the compiler keeps
+      // the read-ahead.
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = (b & 1) * 8 + 2 * i;
-          w[4 * b + i] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(sc[b >> 1][at], kc[b], add)),
-                                     __builtin_amdgcn_exp2f(fmaf(sc[b >> 1][at + 1], kc[b], add)));
-          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[4 * b + i]), ones, sum, false);
+      for (int i = 0; i < N; ++i) {
+        if (i < NPV) {
+          const int b = i / DT;
+          const bf16x8 pk = __builtin_bit_cast(bf16x8, u32x4{w[4 * b], w[4 * b + 1], w[4 * b + 2], w[4 * b + 3]});
+          oacc[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % RA], pk, oacc[i % DT], 0, 0, 0);
+        } else {
+          const int q = i - NPV;
+          sc[q & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % RA], qf[q >> 1], q < 2 ? f32x16{} : sc[q & 1], 0, 0, 0);
         }
-        l = fmaf(sum, vinv[b], l);
+        if (i + RA < N) op[i % RA] = i + RA < NPV ? rdv(vb, i + RA) : rdk(kb, i + RA - NPV);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        const bf16x8 pk = __builtin_bit_cast(bf16x8, u32x4{w[4 * b], w[4 * b + 1], w[4 * b + 2], w[4 * b + 3]});
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-          oacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rdv(base, b, t), pk, oacc[t], 0, 0, 0);
-      }
-      __syncthreads();
+      __builtin_amdgcn_s_setprio(0);
+      stage(st2);
+      const int st = st0;
+      st0 = st1;
+      st1 = st2;
+      st2 = st;
+      read_scales();   // (of the next step: written a step ago)
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      barrier();
     }
 
-    // ---- output: 64 columns at a time through the wave's own area, so that whole lines are stored
+    // ---- the entry's end (part of the next softmax interval): 64 columns at a time through the
+    // wave's own area, so that whole lines are stored
     const float total = sum_pair32(l);
-    const float inv = row_ok ? 1.f / total : 0.f;
-    uint8_t* const stg = lds + 2 * G::STAGE + wave * G::OUT;
+    const float inv = has_row(cur) ? 1.f / total : 0.f;
+    uint8_t* const stg = lds + RING * G::STAGE + wave * G::OUT;
     constexpr int OP = 64 * 2 + 16;
 #pragma unroll
     for (int rd = 0; rd < D / 64; ++rd) {
@@ -301,7 +426,15 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
                                     (lane & 7) * 8) = x;
       }
     }
+    if (!more) break;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) oacc[t] = f32x16{};
+    l = 0.f;
+    e_cur += grid;
+    cur = next;
+    next = fetch(e_cur + grid);
   }
+  if (!group1) barrier();
 }
 
 }  // namespace
