@@ -730,35 +730,57 @@ FP8 = torch.float8_e4m3fn
 FP8_GROUP = 128    # columns of an 8-bit row (and rows of 8-bit weights) that share a scale
 
 
-def _rows(t: torch.Tensor, dtype, name: str, dim: int) -> tuple[int, int]:
-    """(address, elements from one row to the next) of a tensor whose rows are
-    contiguous and may lie apart (a slice of the columns of a larger one)."""
+def _device(t: torch.Tensor, name: str) -> int:
+    """The index of the GPU that a call's first tensor lies on, which must be the
+    current one (whose stream the call takes)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if not t.is_cuda:
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError(f"{name} must be in GPU memory")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != dim:
-        raise ValueError(f"{name} must have {dim} dimensions, got {t.dim()}")
-    width = 1
-    for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size > 1 and step != width:
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on cuda:{dev}, the current device is cuda:{torch._C._cuda_getDevice()}")
+    return dev
+
+
+def _arg(t: torch.Tensor, dtype, name: str, dev: int) -> int:
+    """The address of a contiguous tensor of the given type on GPU `dev` (a kernel
+    would fault on another GPU's memory)."""
+    if isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype is dtype and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, dtype, name)   # names what is wrong
+    raise ValueError(f"{name} is on {t.device}, the call's other tensors are on cuda:{dev}")
+
+
+def _rows(t: torch.Tensor, dtype, name: str, dev: int) -> tuple[int, int]:
+    """(address, elements from one row to the next) of a tensor [rows, width] or
+    [rows, heads, width] on GPU `dev` whose rows are contiguous and may lie apart
+    (a slice of the columns of a larger one)."""
+    shape, step = t.shape, t.stride()
+    width = shape[-1]
+    if step[-1] != 1 and width != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if len(shape) == 3:
+        if step[1] != width and shape[1] != 1:
             raise ValueError(f"{name}: the elements of a row must be contiguous")
-        width *= size
-    if t.shape[0] > 1 and t.stride(0) < width:
+        width *= shape[1]
+    if t.get_device() != dev or t.dtype is not dtype:
+        _dev(t[:0], dtype, name)
+        raise ValueError(f"{name} is on {t.device}, the call's other tensors are on cuda:{dev}")
+    if shape[0] <= 1:
+        return t.data_ptr(), width
+    if step[0] < width:
         raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else width)
+    return t.data_ptr(), step[0]
 
 
-def _same_device(first: torch.Tensor, *others) -> None:
-    """The tensors of a call lie on one GPU, the current one (whose stream the
-    call takes): kernels would fault on another GPU's memory."""
-    if first.is_cuda and first.device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {first.device}, the current device is cuda:{torch.cuda.current_device()}")
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors on {first.device} and {t.device}")
+def _stream_of(stream, dev: int) -> int:
+    """The raw stream: the current one of GPU `dev`, or the given one, which must be dev's."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"the stream is of cuda:{stream.device_index}, the tensors are on cuda:{dev}")
+    return int(stream.cuda_stream)
 
 
 class Fp8KvCache:
@@ -786,12 +808,13 @@ class Fp8KvCache:
     def num_blocks(self) -> int:
         return int(self.k.shape[0])
 
-    def _args(self, num_kv_heads: int, head_dim: int):
+    def _args(self, num_kv_heads: int, head_dim: int, dev: int):
         if self.k.shape[1:] != (num_kv_heads, BLOCK_SIZE, head_dim):
             raise ValueError(f"the cache holds {self.k.shape[1]} KV heads of {self.k.shape[3]}, "
                              f"the call has {num_kv_heads} of {head_dim}")
-        return (_dev(self.k, FP8, "cache.k"), _dev(self.v, FP8, "cache.v"),
-                _dev(self.k_scale, torch.float32, "cache.k_scale"), _dev(self.v_scale, torch.float32, "cache.v_scale"))
+        f32 = torch.float32
+        return (_arg(self.k, FP8, "cache.k", dev), _arg(self.v, FP8, "cache.v", dev),
+                _arg(self.k_scale, f32, "cache.k_scale", dev), _arg(self.v_scale, f32, "cache.v_scale", dev))
 
 
 def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor | None = None,
@@ -801,34 +824,40 @@ def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual
     times weight, in 8 bits with a scale per 128 columns. x and residual are bf16
     [rows, hidden] whose rows may lie apart. Returns (out8, scales, h); h is x
     itself without a residual, else residual_out (which may be x or residual)."""
-    px, sx = _rows(x, torch.bfloat16, "x", 2)
-    T, H = x.shape
-    pr, sr = (None, 0) if residual is None else _rows(residual, torch.bfloat16, "residual", 2)
-    if residual is not None and residual.shape != x.shape:
-        raise ValueError(f"residual must be [{T}, {H}], got {tuple(residual.shape)}")
+    dev, bf16 = _device(x, "x"), torch.bfloat16
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"x must be [rows, hidden], got {tuple(shape)}")
+    T, H = shape
+    px, sx = _rows(x, bf16, "x", dev)
+    pr, sr, write = None, H, None
+    if residual is not None:
+        if residual.shape != shape:
+            raise ValueError(f"residual must be [{T}, {H}], got {tuple(residual.shape)}")
+        pr, sr = _rows(residual, bf16, "residual", dev)
+    if residual_out is not None:
+        if residual_out.shape != shape:
+            raise ValueError(f"residual_out must be [{T}, {H}]")
+        write = _arg(residual_out, bf16, "residual_out", dev)
+    elif residual is None:
+        residual_out = x
+    else:
+        residual_out = torch.empty((T, H), dtype=bf16, device=x.device)
+        write = residual_out.data_ptr()
     if weight.shape != (H,):
         raise ValueError(f"weight must be [{H}], got {tuple(weight.shape)}")
-    if residual_out is None:
-        residual_out = x if residual is None else torch.empty((T, H), dtype=torch.bfloat16, device=x.device)
-        write = residual is not None
-    else:
-        write = True
-        if residual_out.shape != x.shape:
-            raise ValueError(f"residual_out must be [{T}, {H}]")
     groups = -(-H // FP8_GROUP)
     if out8 is None:
         out8 = torch.empty((T, H), dtype=FP8, device=x.device)
-    elif out8.shape != x.shape:
+    elif out8.shape != shape:
         raise ValueError(f"out8 must be [{T}, {H}]")
     if scales is None:
         scales = torch.empty((T, groups), dtype=torch.float32, device=x.device)
     elif scales.shape != (T, groups):
         raise ValueError(f"scales must be [{T}, {groups}]")
-    _same_device(x, residual, weight, residual_out, out8, scales)
-    _check(_lib.cw_add_rms_norm_fp8(
-        px, max(sx, H), pr, max(sr, H), _dev(weight, torch.bfloat16, "weight"), float(eps), T, H,
-        _dev(residual_out, torch.bfloat16, "residual_out") if write else None, _dev(out8, FP8, "out8"),
-        _dev(scales, torch.float32, "scales"), _stream(stream)))
+    _check(_lib.cw_add_rms_norm_fp8(px, sx, pr, sr, _arg(weight, bf16, "weight", dev), eps, T, H, write,
+                                    _arg(out8, FP8, "out8", dev), _arg(scales, torch.float32, "scales", dev),
+                                    _stream_of(stream, dev)))
     return out8, scales, residual_out
 
 
@@ -852,11 +881,11 @@ def fp8_linear(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w_scal
         out = torch.empty((T, N), dtype=torch.bfloat16, device=x8.device)
     elif out.shape != (T, N):
         raise ValueError(f"out must be [{T}, {N}]")
-    _same_device(x8, x_scale, w8, w_scale, bias, out)
-    _check(_lib.cw_fp8_linear(_dev(x8, FP8, "x8"), _dev(x_scale, torch.float32, "x_scale"), _dev(w8, FP8, "w8"),
-                              _dev(w_scale, torch.float32, "w_scale"),
-                              None if bias is None else _dev(bias, torch.bfloat16, "bias"), T, N, K,
-                              _dev(out, torch.bfloat16, "out"), _stream(stream)))
+    dev, f32 = _device(x8, "x8"), torch.float32
+    _check(_lib.cw_fp8_linear(_arg(x8, FP8, "x8", dev), _arg(x_scale, f32, "x_scale", dev), _arg(w8, FP8, "w8", dev),
+                              _arg(w_scale, f32, "w_scale", dev),
+                              None if bias is None else _arg(bias, torch.bfloat16, "bias", dev), T, N, K,
+                              _arg(out, torch.bfloat16, "out", dev), _stream_of(stream, dev)))
     return out
 
 
@@ -871,7 +900,7 @@ def rope_append_fp8(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp
     any."""
     if DEBUG_CHECK_COPIES:
         meta.check_device_copies()
-    hq, hkv, D, T = meta.num_q_heads, meta.num_kv_heads, meta.head_dim, meta.total_rows
+    hq, hkv, D, T = meta.num_q_heads, meta.num_kv_heads, meta.head_dim, int(meta.cu_host[-1])
     for name, t, h in (("q", q, hq), ("k", k, hkv), ("v", v, hkv)):
         if t is not None and t.shape != (T, h, D):
             raise ValueError(f"{name} must be [{T}, {h}, {D}], got {tuple(t.shape)}")
@@ -883,18 +912,17 @@ def rope_append_fp8(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp
         q_out = torch.empty((T, hq, D), dtype=torch.bfloat16, device=q.device)
     elif q_out is not None and q_out.shape != (T, hq, D):
         raise ValueError(f"q_out must be [{T}, {hq}, {D}]")
-    pk, sk = _rows(k, torch.bfloat16, "k", 3)
-    pv, sv = _rows(v, torch.bfloat16, "v", 3)
-    pq, sq = (None, 0) if q is None else _rows(q, torch.bfloat16, "q", 3)
-    _same_device(cache.k, k, v, q, rope, q_out, cache.v, cache.k_scale, cache.v_scale, meta.bt, meta.cu, meta.plen)
-    ck, cv, cks, cvs = cache._args(hkv, D)
+    dev, bf16, i32 = _device(cache.k, "cache.k"), torch.bfloat16, torch.int32
+    pk, sk = _rows(k, bf16, "k", dev)
+    pv, sv = _rows(v, bf16, "v", dev)
+    pq, sq = (None, 0) if q is None else _rows(q, bf16, "q", dev)
+    ck, cv, cks, cvs = cache._args(hkv, D, dev)
     _check(_lib.cw_rope_append_fp8(
-        pq, max(sq, hq * D), pk, max(sk, hkv * D), pv, max(sv, hkv * D),
-        None if rope is None else _dev(rope, torch.float32, "rope"), 0 if rope is None else int(rope.shape[0]),
-        None if q_out is None else _dev(q_out, torch.bfloat16, "q_out"), ck, cv, cks, cvs,
-        _dev(meta.bt, torch.int32, "block_table"), meta.bt_stride, _dev(meta.cu, torch.int32, "cu_suffix"),
-        _dev(meta.plen, torch.int32, "prefix_len"), meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch,
-        hq, hkv, D, BLOCK_SIZE, cache.num_blocks, _stream(stream)))
+        pq, sq, pk, sk, pv, sv, None if rope is None else _arg(rope, torch.float32, "rope", dev),
+        0 if rope is None else rope.shape[0], None if q_out is None else _arg(q_out, bf16, "q_out", dev), ck, cv, cks,
+        cvs, _arg(meta.bt, i32, "block_table", dev), meta.bt_stride, _arg(meta.cu, i32, "cu_suffix", dev),
+        _arg(meta.plen, i32, "prefix_len", dev), meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv,
+        D, BLOCK_SIZE, cache.k.shape[0], _stream_of(stream, dev)))
     return q_out
 
 
@@ -911,12 +939,12 @@ def suffix_prefill_attn_fp8(meta: BatchMeta, q: torch.Tensor, cache: Fp8KvCache,
         out = torch.empty_like(q)
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
-    _same_device(cache.k, q, out, cache.v, cache.k_scale, cache.v_scale, meta.bt, meta.plan)
+    dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
     _check(_lib.cw_suffix_prefill_attn_fp8(
-        _dev(q, torch.bfloat16, "q"), *cache._args(hkv, D), _dev(meta.bt, torch.int32, "block_table"),
-        meta.bt_stride, meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE,
-        cache.num_blocks, float(softmax_scale), meta._hp(meta.plan_host), _dev(meta.plan, torch.int32, "plan"),
-        _dev(out, torch.bfloat16, "out"), _stream(stream)))
+        _arg(q, bf16, "q", dev), *cache._args(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
+        meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.k.shape[0],
+        softmax_scale, meta._hp(meta.plan_host), _arg(meta.plan, i32, "plan", dev), _arg(out, bf16, "out", dev),
+        _stream_of(stream, dev)))
     return out
 
 
@@ -960,12 +988,12 @@ def decode_attn_fp8(q: torch.Tensor, cache: Fp8KvCache, block_table: torch.Tenso
     need = decode_workspace_bytes(B, hq, D, num_splits)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _same_device(cache.k, q, out, block_table, seq_lens, cache.v, cache.k_scale, cache.v_scale, workspace)
+    dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
     _check(_lib.cw_decode_attn_fp8(
-        _dev(q, torch.bfloat16, "q"), *cache._args(hkv, D), _dev(block_table, torch.int32, "block_table"), stride,
-        _dev(seq_lens, torch.int32, "seq_lens"), B, hq, hkv, D, BLOCK_SIZE, cache.num_blocks, float(softmax_scale),
-        int(num_splits), None if workspace is None else _dev(workspace, torch.uint8, "workspace"),
-        0 if workspace is None else workspace.numel(), _dev(out, torch.bfloat16, "out"), _stream(stream)))
+        _arg(q, bf16, "q", dev), *cache._args(hkv, D, dev), _arg(block_table, i32, "block_table", dev), stride,
+        _arg(seq_lens, i32, "seq_lens", dev), B, hq, hkv, D, BLOCK_SIZE, cache.k.shape[0], softmax_scale, num_splits,
+        None if workspace is None else _arg(workspace, torch.uint8, "workspace", dev),
+        0 if workspace is None else workspace.numel(), _arg(out, bf16, "out", dev), _stream_of(stream, dev)))
     return out
 
 

@@ -675,7 +675,7 @@ def test_python_refusals_on_the_gpu():
     with pytest.raises(TypeError, match="float8"):
         cw.fp8_linear(k.view(8, 64), torch.ones(8, 1).cuda(), k.view(8, 64), torch.ones(1, 1).cuda())
     x = torch.zeros(2, 64, dtype=torch.bfloat16, device="cuda")
-    with pytest.raises(ValueError, match="tensors on"):
+    with pytest.raises(ValueError, match="GPU memory"):
         cw.add_rms_norm_fp8(x, torch.zeros(64, dtype=torch.bfloat16), 1e-5)
     with pytest.raises(cw.CwError, match="hidden must be a multiple"):
         cw.add_rms_norm_fp8(torch.zeros(2, 24, dtype=torch.bfloat16, device="cuda"),
