@@ -630,6 +630,42 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_fp8_kernel(const Deco
   }
 }
 
+// Joins the runs of a row: M = max_p lse_p, out = sum_p 2^(lse_p - M) o_p / sum_p 2^(lse_p - M). One
+// workgroup per row, D / 4 columns of 4 values x 1024 / D groups of runs. Rows are few and runs up to 64
+// (one lane each), so it is bound by latency: the runs' values are loaded with their sums, all of a
+// thread's at once. (A run without keys is written as zeros with -inf.) 32 rows of 128, 24 runs, with
+// the attention before it: 11.4 us, 19.1 with lse_merge_kernel, which takes the runs in turn; 4,096 rows, 2 to
+// 8 runs: 7 us.
+template <int D>
+__global__ __launch_bounds__(kThreads) void decode_join_kernel(const float* part_o, const float* part_lse, int parts,
+                                                               int64_t rows, uint16_t* out) {
+  constexpr int COLS = D / 4, NG = kThreads / COLS;
+  constexpr int MOST = cw::kMaxSplits / NG;
+  __shared__ __attribute__((aligned(16))) f32x4 s_acc[NG][COLS];
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 63, c = threadIdx.x % COLS, g = threadIdx.x / COLS;
+  const float lse = lane < parts ? part_lse[lane * rows + row] : -INFINITY;
+  f32x4 v[MOST];
+#pragma unroll
+  for (int i = 0; i < MOST; ++i) {
+    const int p = g + i * NG;
+    v[i] = p < parts ? *reinterpret_cast<const f32x4*>(part_o + (p * rows + row) * D + 4 * c) : f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float M = wave_max(lse);
+  const float w = lse != -INFINITY ? __builtin_amdgcn_exp2f(lse - M) : 0.f;   // (NaN stays one)
+  const float sum = wave_sum(w);
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < MOST; ++i) acc += __shfl(w, min(g + i * NG, 63)) * v[i];
+  s_acc[g][c] = acc;
+  __syncthreads();
+  if (g > 0) return;
+#pragma unroll
+  for (int i = 1; i < NG; ++i) acc += s_acc[i][c];
+  acc *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+  *reinterpret_cast<u32x2*>(out + row * D + 4 * c) = u32x2{pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
+}
+
 cw_status check_launch(const char* what) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return cw::fail(CW_EHIP, std::string(what) + ": " + hipGetErrorString(e));
@@ -823,7 +859,7 @@ extern "C" cw_status cw_decode_attn_fp8(const void* q, const void* k8, const voi
   a.head_tiles = (a.group + kTileHeads - 1) / kTileHeads;
   a.c_log2 = softmax_scale * 1.4426950408889634f;
   const int64_t grid = int64_t(batch) * num_kv_heads * a.head_tiles * num_splits;
-  if (grid > INT32_MAX) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
+  if (grid > INT32_MAX || rows > INT32_MAX) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
   auto* const s = static_cast<hipStream_t>(stream);
   if (head_dim == 128)
     hipLaunchKernelGGL(decode_attn_fp8_kernel<128>, dim3(unsigned(grid)), dim3(kThreads), 0, s, a);
@@ -831,5 +867,11 @@ extern "C" cw_status cw_decode_attn_fp8(const void* q, const void* k8, const voi
     hipLaunchKernelGGL(decode_attn_fp8_kernel<64>, dim3(unsigned(grid)), dim3(kThreads), 0, s, a);
   st = check_launch("decode_attn_fp8 launch");
   if (st != CW_OK || num_splits == 1) return st;
-  return cw_lse_merge(a.part_o, a.part_lse, num_splits, rows, head_dim, out, stream);
+  if (head_dim == 128)
+    hipLaunchKernelGGL(decode_join_kernel<128>, dim3(unsigned(rows)), dim3(kThreads), 0, s, a.part_o, a.part_lse,
+                       num_splits, rows, a.out);
+  else
+    hipLaunchKernelGGL(decode_join_kernel<64>, dim3(unsigned(rows)), dim3(kThreads), 0, s, a.part_o, a.part_lse,
+                       num_splits, rows, a.out);
+  return check_launch("decode_attn_fp8 join launch");
 }
