@@ -783,10 +783,12 @@ extern "C" cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const v
   a.hkv = num_kv_heads;
   a.num_blocks = num_blocks;
   a.rope_len = rope_len;
-  // Heads over grid y: enough waves for the chip, then as many heads a wave as there are
-  // (they share the rows' cosines and sines).
+  // Heads over grid y: a workgroup per CU at least, and two per unit, so that the last round of a
+  // large batch is short; more share the rows' cosines and sines less. us for 1, 2, 3, 4, 6, 12 per unit:
+  // 1,030 units of 48 heads 93.6, 87.6, 88.4, 96.2, 88.7, 108.1; 64 units 14.9, 9.4, 8.4, 6.9, 7.4, 7.8;
+  // 160 units of 36 heads 14.1, 12.5, 11.7, 12.9, 12.5, 14.2.
   const int64_t heads = a.hq + 2 * int64_t(num_kv_heads), full = (heads + kWaves - 1) / kWaves;
-  const int64_t gy = std::min(std::min<int64_t>(full, 65535), std::max<int64_t>(1, 2048 / units));
+  const int64_t gy = std::min({full, int64_t(65535), std::max<int64_t>(2, (cw::kNumCu + units - 1) / units)});
   auto* const s = static_cast<hipStream_t>(stream);
   if (head_dim == 128)
     hipLaunchKernelGGL(rope_append_fp8_kernel<128>, dim3(unsigned(units), unsigned(gy)), dim3(kThreads), 0, s, a);
