@@ -533,7 +533,9 @@ cw_status cw_qkv_rope_append(const void* x, const void* w, const void* bias, con
  * (scale 1 and zeros where max|h * weight| of the columns is below 2^-100, or below
  * 2^-68 in a row whose sum of squares is above fp32). A row of h with an infinity or
  * a NaN has NaN codes and scales 1; columns whose weight is infinite or NaN have
- * NaN codes, and the scale comes from the others.
+ * NaN codes, and the scale comes from the others. |h * weight| must stay below 2^119
+ * (2^151 where the sum of squares is above fp32): what passes it has NaN codes, and the
+ * codes of its 128 columns are not defined.
  *   x, residual    device bf16 [rows, hidden], rows x_stride / residual_stride
  *                  elements apart
  *   weight         device bf16 [hidden]
@@ -542,8 +544,9 @@ cw_status cw_qkv_rope_append(const void* x, const void* w, const void* bias, con
  *   out8           device e4m3 [rows, hidden]
  *   scales         device fp32 [rows, ceil(hidden / 128)]
  * CW_EINVAL: NULL pointer, rows < 0, eps outside [1e-20, 1], a stride below
- * hidden or no multiple of 8, a misaligned pointer. CW_EUNSUPPORTED: hidden not
- * a multiple of 16 in [16, 16384], more than 2^31 - 1 rows. CW_EHIP: launch. */
+ * hidden or no multiple of 8, residual_out at the address of rows that lie apart, a
+ * misaligned pointer. CW_EUNSUPPORTED: hidden not a multiple of 16 in [16, 16384],
+ * more than 2^22 rows. CW_EHIP: launch. */
 cw_status cw_add_rms_norm_fp8(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
                               const void* weight, float eps, int64_t rows, int32_t hidden, void* residual_out,
                               void* out8, float* scales, void* stream);
@@ -561,7 +564,8 @@ cw_status cw_add_rms_norm_fp8(const void* x, int64_t x_stride, const void* resid
  *   bias     device bf16 [features], or NULL for none
  *   out      device bf16 [rows, features]
  * CW_EINVAL: NULL pointer, rows < 0, a misaligned pointer. CW_EUNSUPPORTED:
- * hidden or features not a multiple of 16 in [16, 2^20], more than 2^22 rows.
+ * hidden or features not a multiple of 16 in [16, 2^20], more than 2^22 rows, more
+ * tiles than a launch holds.
  * CW_EHIP: launch failure. */
 cw_status cw_fp8_linear(const void* x8, const float* x_scale, const void* w8, const float* w_scale,
                         const void* bias, int64_t rows, int32_t features, int32_t hidden, void* out, void* stream);
@@ -611,7 +615,8 @@ cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const void* k, int
  * Device: cw_suffix_prefill_attn over the 8-bit cache, which must already hold
  * prefix and suffix. Keys and values are code * scale, exactly; q and out are
  * bf16. Probabilities times their value's scale are rounded to bf16 for the
- * product with the codes; softmax and sums are fp32.
+ * product with the codes; softmax and sums are fp32, before the division by the
+ * probabilities' sum: values above 2^96 in magnitude may overflow them.
  *   plan_host / plan_dev   the unsplit plan of cw_suffix_prefill_plan
  * A table entry outside [0, num_blocks) is read as zero keys and values, each
  * with score 0. A NaN code of a visible key or value makes the outputs that see
@@ -633,7 +638,7 @@ cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, const void* 
  * Lengths are read from device memory alone, and the launch does not depend on
  * them: a captured call can be replayed as sequences grow. A length above
  * 16 * bt_stride counts as that, one below 0 as 0. Table entries outside the
- * pool and NaN codes as for cw_suffix_prefill_attn_fp8.
+ * pool, NaN codes and values above 2^96 as for cw_suffix_prefill_attn_fp8.
  *   q, out       device bf16 [batch, Hq, D]
  *   seq_lens_dev device int32 [batch]
  *   num_splits   1 .. 64 runs that each sequence is cut into, combined as by

@@ -30,6 +30,7 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kBs = cw::kBlockSize;
 constexpr float kFp8Max = 448.f;
 constexpr int kGroupCols = 128;   // columns of an 8-bit row that share a scale
+constexpr int64_t kMaxGrid = UINT32_MAX / kThreads;   // a launch has fewer than 2^32 threads along an axis
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -693,9 +694,12 @@ extern "C" cw_status cw_add_rms_norm_fp8(const void* x, int64_t x_stride, const 
   if (!(eps >= 1e-20f && eps <= 1.f)) return cw::fail(CW_EINVAL, "add_rms_norm_fp8: eps must be in [1e-20, 1]");
   if (hidden < 16 || hidden % 16 != 0 || hidden > 16384)
     return cw::fail(CW_EUNSUPPORTED, "add_rms_norm_fp8: hidden must be a multiple of 16 in [16, 16384]");
-  if (rows > INT32_MAX) return cw::fail(CW_EUNSUPPORTED, "add_rms_norm_fp8: too many rows");
+  if (rows > (1 << 22)) return cw::fail(CW_EUNSUPPORTED, "add_rms_norm_fp8: more than 2^22 rows");
   if (x_stride < hidden || x_stride % 8 != 0 || (residual && (residual_stride < hidden || residual_stride % 8 != 0)))
     return cw::fail(CW_EINVAL, "add_rms_norm_fp8: row strides must be multiples of 8, at least hidden");
+  if (rows > 1 && residual_out && ((residual_out == x && x_stride != hidden) ||
+                                   (residual_out == residual && residual_stride != hidden)))
+    return cw::fail(CW_EINVAL, "add_rms_norm_fp8: residual_out is contiguous: it cannot be rows that lie apart");
   if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(residual_out) || !aligned16(out8))
     return cw::fail(CW_EINVAL, "add_rms_norm_fp8: pointers must be 16-byte aligned");
   if (rows == 0) return cw::ok();
@@ -760,7 +764,7 @@ extern "C" cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const v
     return cw::fail(CW_EINVAL, w + ": rope_len " + std::to_string(rope_len) + " is below the longest prompt (" +
                                    std::to_string(longest) + ")");
   if (rows == 0) return cw::ok();
-  if (units > INT32_MAX) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
+  if (units > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
   AppendArgs a;
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
@@ -861,7 +865,7 @@ extern "C" cw_status cw_decode_attn_fp8(const void* q, const void* k8, const voi
   a.head_tiles = (a.group + kTileHeads - 1) / kTileHeads;
   a.c_log2 = softmax_scale * 1.4426950408889634f;
   const int64_t grid = int64_t(batch) * num_kv_heads * a.head_tiles * num_splits;
-  if (grid > INT32_MAX || rows > INT32_MAX) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
+  if (grid > kMaxGrid || rows > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
   auto* const s = static_cast<hipStream_t>(stream);
   if (head_dim == 128)
     hipLaunchKernelGGL(decode_attn_fp8_kernel<128>, dim3(unsigned(grid)), dim3(kThreads), 0, s, a);

@@ -636,11 +636,12 @@ extern "C" cw_status cw_fp8_linear(const void* x8, const float* x_scale, const v
   a.n_ftiles = (features + sh.tile_f - 1) / sh.tile_f;
   a.n_ttiles = int((rows + sh.tile_t - 1) / sh.tile_t);
   const int64_t per_xcd = (int64_t(a.n_ftiles) * a.n_ttiles + cw::kNumXcd - 1) / cw::kNumXcd;
-  if (per_xcd * cw::kNumXcd > INT32_MAX) return cw::fail(CW_EUNSUPPORTED, "fp8_linear: too many tiles");
-  a.per_xcd = int(per_xcd);
   const int64_t grid = (sh.persistent ? std::min<int64_t>(per_xcd, cw::kNumCu / cw::kNumXcd) : per_xcd) * cw::kNumXcd;
-  hipLaunchKernelGGL(sh.kernel, dim3(unsigned(grid)), dim3(512), 0, static_cast<hipStream_t>(stream),
-                     a);
+  // (a launch has fewer than 2^32 threads; the kernels count tiles in 32 bits)
+  if (grid > UINT32_MAX / 512 || per_xcd * cw::kNumXcd > INT32_MAX)
+    return cw::fail(CW_EUNSUPPORTED, "fp8_linear: too many tiles");
+  a.per_xcd = int(per_xcd);
+  hipLaunchKernelGGL(sh.kernel, dim3(unsigned(grid)), dim3(512), 0, static_cast<hipStream_t>(stream), a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return cw::fail(CW_EHIP, std::string("fp8_linear launch: ") + hipGetErrorString(e));
   return cw::ok();

@@ -756,6 +756,8 @@ def _rows(t: torch.Tensor, dtype, name: str, dev: int) -> tuple[int, int]:
     """(address, elements from one row to the next) of a tensor [rows, width] or
     [rows, heads, width] on GPU `dev` whose rows are contiguous and may lie apart
     (a slice of the columns of a larger one)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
     shape, step = t.shape, t.stride()
     width = shape[-1]
     if step[-1] != 1 and width != 1:
@@ -781,6 +783,15 @@ def _stream_of(stream, dev: int) -> int:
     if stream.device_index != dev:
         raise ValueError(f"the stream is of cuda:{stream.device_index}, the tensors are on cuda:{dev}")
     return int(stream.cuda_stream)
+
+
+def _new(stream, shape, dtype, device) -> torch.Tensor:
+    """A result or workspace of a call on `stream`, allocated for that stream: its memory may
+    still be in use by what the current stream does, or be given to it once it is freed."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 class Fp8KvCache:
@@ -842,17 +853,17 @@ def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual
     elif residual is None:
         residual_out = x
     else:
-        residual_out = torch.empty((T, H), dtype=bf16, device=x.device)
+        residual_out = _new(stream, (T, H), bf16, x.device)
         write = residual_out.data_ptr()
     if weight.shape != (H,):
         raise ValueError(f"weight must be [{H}], got {tuple(weight.shape)}")
     groups = -(-H // FP8_GROUP)
     if out8 is None:
-        out8 = torch.empty((T, H), dtype=FP8, device=x.device)
+        out8 = _new(stream, (T, H), FP8, x.device)
     elif out8.shape != shape:
         raise ValueError(f"out8 must be [{T}, {H}]")
     if scales is None:
-        scales = torch.empty((T, groups), dtype=torch.float32, device=x.device)
+        scales = _new(stream, (T, groups), torch.float32, x.device)
     elif scales.shape != (T, groups):
         raise ValueError(f"scales must be [{T}, {groups}]")
     _check(_lib.cw_add_rms_norm_fp8(px, sx, pr, sr, _arg(weight, bf16, "weight", dev), eps, T, H, write,
@@ -878,7 +889,7 @@ def fp8_linear(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w_scal
     if bias is not None and bias.shape != (N,):
         raise ValueError(f"bias must be [{N}], got {tuple(bias.shape)}")
     if out is None:
-        out = torch.empty((T, N), dtype=torch.bfloat16, device=x8.device)
+        out = _new(stream, (T, N), torch.bfloat16, x8.device)
     elif out.shape != (T, N):
         raise ValueError(f"out must be [{T}, {N}]")
     dev, f32 = _device(x8, "x8"), torch.float32
@@ -909,7 +920,7 @@ def rope_append_fp8(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp
     if q is None and q_out is not None:
         raise ValueError("q_out without q")
     if q is not None and q_out is None:
-        q_out = torch.empty((T, hq, D), dtype=torch.bfloat16, device=q.device)
+        q_out = _new(stream, (T, hq, D), torch.bfloat16, q.device)
     elif q_out is not None and q_out.shape != (T, hq, D):
         raise ValueError(f"q_out must be [{T}, {hq}, {D}]")
     dev, bf16, i32 = _device(cache.k, "cache.k"), torch.bfloat16, torch.int32
@@ -936,7 +947,7 @@ def suffix_prefill_attn_fp8(meta: BatchMeta, q: torch.Tensor, cache: Fp8KvCache,
     if q.shape != (meta.total_rows, hq, D):
         raise ValueError(f"q must be [{meta.total_rows}, {hq}, {D}], got {tuple(q.shape)}")
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, q.shape, torch.bfloat16, q.device)
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
     dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
@@ -973,7 +984,8 @@ def decode_attn_fp8(q: torch.Tensor, cache: Fp8KvCache, block_table: torch.Tenso
     the first seq_lens [batch] (int32, device) tokens of its row of block_table
     [batch, stride] (int32, device); returns out [batch, Hq, D] bf16. `workspace`
     (uint8, device) is allocated when not given; calls that may run at the same
-    time, captured ones among them, need one each."""
+    time, captured ones among them, need one each. What a call of this section
+    allocates belongs to its stream."""
     if q.dim() != 3:
         raise ValueError(f"q must be [batch, Hq, D], got {tuple(q.shape)}")
     B, hq, D = q.shape
@@ -983,15 +995,17 @@ def decode_attn_fp8(q: torch.Tensor, cache: Fp8KvCache, block_table: torch.Tenso
     if seq_lens.shape != (B,):
         raise ValueError(f"seq_lens must be [{B}], got {tuple(seq_lens.shape)}")
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, q.shape, torch.bfloat16, q.device)
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
     stride = int(block_table.shape[1])
+    if hkv < 1:
+        raise ValueError("the cache has no KV heads")
     if num_splits is None:
         num_splits = decode_split_count(B, hq, hkv, stride * BLOCK_SIZE)
     need = decode_workspace_bytes(B, hq, D, num_splits)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _new(stream, need, torch.uint8, q.device)
     dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
     _check(_lib.cw_decode_attn_fp8(
         _arg(q, bf16, "q", dev), *cache._args(hkv, D, dev), _arg(block_table, i32, "block_table", dev), stride,

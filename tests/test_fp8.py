@@ -107,11 +107,16 @@ def _norm(x=d_, xs=64, r=d_, rs=64, w=d_, eps=1e-5, rows=4, hidden=64, ro=d_, o=
     (E, dict(rows=-1)), (E, dict(x=None)), (E, dict(w=None)), (E, dict(o=None)), (E, dict(s=None)), (E, dict(eps=0.0)),
     (E, dict(eps=float("nan"))), (E, dict(eps=2.0)), (E, dict(xs=56)), (E, dict(xs=68)), (E, dict(rs=56)),
     (E, dict(x=odd)), (E, dict(ro=odd)), (E, dict(o=odd)), (U, dict(hidden=24, xs=64)), (U, dict(hidden=0)),
-    (U, dict(hidden=16400, xs=16400, rs=16400)), (U, dict(rows=2 ** 31)),
+    (U, dict(hidden=16400, xs=16400, rs=16400)), (U, dict(rows=2 ** 31)), (U, dict(rows=2 ** 22 + 1)),
 ])
 def test_norm_refusals(status, change):
     assert _norm(**change) == status
     assert "add_rms_norm_fp8" in cw.last_error()
+
+
+@pytest.mark.parametrize("change", [dict(ro=d_, x=d_, xs=72, r=None), dict(ro=d_, r=d_, rs=128, x=ctypes.c_void_p(8192))])
+def test_norm_in_place_only_where_rows_are_contiguous(change):
+    assert _norm(**change) == E and "rows that lie apart" in cw.last_error()
 
 
 def test_norm_of_no_rows_launches_nothing():
@@ -194,7 +199,7 @@ def _decode(q=d_, k8=d_, v8=d_, sk=d_, sv=d_, bt=d_, stride=4, lens=d_, batch=2,
     (E, dict(nb=0)), (E, dict(scale=-1.0)), (E, dict(scale=float("nan"))), (E, dict(splits=0)), (E, dict(splits=65)),
     (E, dict(splits=2)), (E, dict(splits=2, ws=d_, wb=2 * 16 * 65 * 4 - 1)), (E, dict(splits=2, ws=odd, wb=1 << 20)),
     (E, dict(q=odd)), (E, dict(out=odd)), (E, dict(k8=odd)), (U, dict(d=32)), (U, dict(bs=32)), (U, dict(hq=2 * 129)),
-    (U, dict(stride=2 ** 27)), (U, dict(batch=2 ** 30, splits=1)),
+    (U, dict(stride=2 ** 27)), (U, dict(batch=2 ** 30, splits=1)), (U, dict(batch=2 ** 23, splits=1)),
 ])
 def test_decode_refusals(status, change):
     assert _decode(**change) == status
@@ -241,3 +246,9 @@ def test_python_argument_checks():
         cw.rope_append_fp8(meta, q, q, cache)
     with pytest.raises(ValueError, match="q must be"):
         cw.suffix_prefill_attn_fp8(meta, q[:1], cache, 0.1)
+    with pytest.raises(ValueError, match="no KV heads"):
+        cw.decode_attn_fp8(q, cw.Fp8KvCache(4, 0, 64, device="cpu"), torch.zeros(2, 4, dtype=torch.int32),
+                           torch.zeros(2, dtype=torch.int32), 0.1)
+    with pytest.raises(TypeError, match="k must be a torch tensor"):
+        cw._rows(None, torch.bfloat16, "k", 0)
+

@@ -221,6 +221,31 @@ def test_linear_rows_alone_equal_rows_in_a_batch():
     assert torch.equal(_bits(one[0]), _bits(all_rows[777]))
 
 
+@pytest.mark.parametrize("rows,hidden,feats", [(4099, 400, 6160), (2100, 2064, 4112), (5000, 1040, 1040),
+                                               (16000, 272, 400), (2000, 4112, 6160)])
+def test_linear_many_rows(rows, hidden, feats):
+    """Large tiles, with several tiles a workgroup, cut rows, features and columns: sampled rows against
+    fp64, and all rows' bits equal to those of the same rows in calls of 96."""
+    _say(f"linear {rows} x {hidden} x {feats}")
+    g = _gen(rows)
+    x8, w8 = _quantised(g, rows, hidden), _quantised(g, feats, hidden)
+    xs, ws = _scales(g, rows, hidden), _scales(g, -(-feats // 128), hidden)
+    b = _normal(g, feats, std=50.0)
+    dev = [t.cuda() for t in (x8, xs, w8, ws, b)]
+    buf = torch.full((rows + 300, feats), 3.0, dtype=torch.bfloat16, device="cuda")
+    got = cw.fp8_linear(*dev, out=buf[:rows])
+    torch.cuda.synchronize()
+    assert (buf[rows:] == 3).all()
+    for t in range(0, rows, 96):
+        part = cw.fp8_linear(dev[0][t:t + 96], dev[1][t:t + 96], *dev[2:])
+        assert torch.equal(part.view(torch.int16), got[t:t + 96].view(torch.int16)), t
+    pick = [0, 1, 255, 256, 1023, rows - 257, rows - 2, rows - 1]
+    exp, mag = F.linear(_f64(x8[pick]), _f64(xs[pick]), _f64(w8), _f64(ws), _f64(b))
+    cut = F.linear_cut(_f64(x8[pick]), _f64(xs[pick]), _f64(w8), _f64(ws))[0]
+    _within(_f64(got[pick]), exp, B8 * np.abs(exp) + (hidden + hidden / 128 + 4) * 2.0 ** -23 * mag + 7 * 2.0 ** -13 * cut,
+            "sampled rows")
+
+
 def test_linear_nan_code_stays_in_its_row():
     g = _gen(10)
     x8 = _quantised(g, 40, 256)
@@ -659,6 +684,109 @@ def test_layer_prefill_then_decode_steps():
             rows = slice(b.cu[i], b.cu[i + 1])
             _check_attention(_f64(out[rows]), _f64(qr[rows]), b.rows(0, i), b.rows(1, i), lens[i], D ** -0.5, what)
         lens = [a + c for a, c in zip(lens, n)]
+
+
+def _layer_inputs(seed, P, S, hq=8, hkv=2, D=64, hidden=272):
+    """A layer's weights, a cache with room, and one call's static inputs."""
+    b = Batch(hq, hkv, D, [p + s for p, s in zip(P, S)], [0] * len(P), seed=seed, spread=0.0, held=P)
+    g, feats, T = b.g, (hq + 2 * hkv) * D, sum(S)
+    meta = cw.BatchMeta(b.bt, np.concatenate([[0], np.cumsum(S)]), P, hq, hkv, D)
+    seq = torch.tensor([p + s for p, s in zip(P, S)], dtype=torch.int32).cuda()
+    w8, ws = _quantised(g, feats, hidden).cuda(), _scales(g, feats // 128, hidden, -12, -11).cuda()
+    weight, rope = torch.ones(hidden, dtype=torch.bfloat16, device="cuda"), torch.from_numpy(cw.rope_table(128, D, 10000.0)).cuda()
+    x, r = torch.zeros(2, T, hidden, dtype=torch.bfloat16, device="cuda").unbind(0)
+
+    def run(cache, stream=None):
+        x8, xs, h = cw.add_rms_norm_fp8(x, weight, 1e-5, residual=r, stream=stream)
+        qkv = cw.fp8_linear(x8, xs, w8, ws, stream=stream)
+        q, k, v = (t.view(T, -1, D) for t in qkv.split([hq * D, hkv * D, hkv * D], 1))
+        qr = cw.rope_append_fp8(meta, k, v, cache, q=q, rope=rope, stream=stream)
+        out = cw.suffix_prefill_attn_fp8(meta, qr, cache, D ** -0.5, stream=stream)
+        last = qr[(meta.cu[1:] - 1).long()] if stream is None else None
+        return [x8.view(torch.uint8), xs, h, qr, out] + (
+            [] if last is None else [cw.decode_attn_fp8(last, cache, meta.bt, seq, D ** -0.5, num_splits=3)])
+
+    return b, x, r, run
+
+
+def _copy_of(cache):
+    return cw.Fp8KvCache.of(cache.k.clone(), cache.v.clone(), cache.k_scale.clone(), cache.v_scale.clone())
+
+
+def test_layer_captured_and_replayed():
+    """The five calls in one captured graph, replayed with other hidden states between eager runs on a copy
+    of the cache: every replay has the eager run's bits, in its results and in the cache."""
+    b, x, r, run = _layer_inputs(51, [20, 0, 37], [9, 17, 1])
+    twin = _copy_of(b.cache)
+    run(_copy_of(b.cache))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        got = run(b.cache)
+    for step in range(4):
+        for t in (x, r):
+            t.copy_(_normal(b.g, *t.shape).cuda())
+        want = [t.clone() for t in run(twin)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, e) in enumerate(zip(got, want)):
+            assert torch.equal(a.view(torch.uint8), e.view(torch.uint8)), (step, i)
+        for n in ("k", "v", "k_scale", "v_scale"):
+            assert torch.equal(getattr(b.cache, n).view(torch.uint8), getattr(twin, n).view(torch.uint8)), (step, n)
+
+
+def test_layer_on_given_streams():
+    """With stream=: two layers' calls on two streams at once equal the ones on the current stream, and what
+    the calls allocate comes from their stream's memory."""
+    sets = [_layer_inputs(seed, [20, 0, 37], [40, 117, 1]) for seed in (52, 53)]
+    for b, x, r, _ in sets:
+        for t in (x, r):
+            t.copy_(_normal(b.g, *t.shape).cuda())
+    want = [run(_copy_of(b.cache)) for b, _, _, run in sets]
+    caches = [_copy_of(b.cache) for b, *_ in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = [run(c, stream=s) for (*_, run), c, s in zip(sets, caches, streams)]
+    torch.cuda.synchronize()
+    for g, w, s in zip(got, want, streams):
+        for i, (a, e) in enumerate(zip(g, w)):
+            assert torch.equal(a.view(torch.uint8), e.view(torch.uint8)), i
+            seg = [m for m in torch.cuda.memory_snapshot()
+                   if m["address"] <= a.data_ptr() < m["address"] + m["total_size"]]
+            assert [m["stream"] for m in seg] == [s.cuda_stream], i
+
+
+def test_decode_calls_at_once_on_two_streams():
+    """Two calls at the same time with workspaces that they allocate themselves."""
+    b = Batch(8, 2, 128, [900, 300], [0, 0], seed=54, spread=0.5)
+    bt = torch.from_numpy(b.bt).cuda()
+    qs = [b.queries(2).cuda() for _ in range(2)]
+    sl = [torch.tensor(n, dtype=torch.int32).cuda() for n in ([900, 300], [850, 1])]
+    want = [cw.decode_attn_fp8(q, b.cache, bt, n, 128 ** -0.5, num_splits=5) for q, n in zip(qs, sl)]
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    got = [[cw.decode_attn_fp8(q, b.cache, bt, n, 128 ** -0.5, num_splits=5, stream=s) for _ in range(8)]
+           for q, n, s in zip(qs, sl, streams)]
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(_bits(t), _bits(w)) for t in g)
+
+
+def test_batches_with_no_rows():
+    """Batches whose requests are all empty launch nothing; the cache keeps its bytes."""
+    b = Batch(8, 2, 64, [20, 0], [0, 0], seed=55)
+    before = b.cache.k.view(torch.uint8).clone()
+    none = torch.empty(0, 8, 64, dtype=torch.bfloat16, device="cuda")
+    kv = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    rope = torch.from_numpy(cw.rope_table(64, 64, 10000.0)).cuda()
+    assert cw.rope_append_fp8(b.meta(), kv, kv, b.cache, q=none, rope=rope).shape == none.shape
+    assert cw.suffix_prefill_attn_fp8(b.meta(), none, b.cache, 0.1).shape == none.shape
+    x8, xs, h = cw.add_rms_norm_fp8(none.view(0, 512), torch.ones(512, dtype=torch.bfloat16, device="cuda"), 1e-5)
+    w8, ws = _quantised(b.g, 48, 512).cuda(), _scales(b.g, 1, 512).cuda()
+    assert cw.fp8_linear(x8, xs, w8, ws).shape == (0, 48)
+    torch.cuda.synchronize()
+    assert torch.equal(before, b.cache.k.view(torch.uint8))
 
 
 def test_python_refusals_on_the_gpu():
