@@ -71,8 +71,8 @@ struct Geom {
   static constexpr int VP = 2 * D + 64;           // the same of V: the 4 rows x 64 bytes that half a wave
                                                   // reads at once (transposing) lie on distinct banks
   static constexpr int KTILE = kStep * KP;
-  static constexpr int SCALES = KTILE + kStep * VP;   // k_scale, then v_scale of the step's blocks (fp32)
-  static constexpr int STAGE = SCALES + 2 * kBlocks * 4;
+  static constexpr int SCALES = KTILE + kStep * VP;   // of the step's blocks, fp32: c k_scale, log2 v_scale, 1 / v_scale
+  static constexpr int STAGE = SCALES + 3 * kBlocks * 4;
   static constexpr int PIECES = kBs * D / 1024;   // 16-byte pieces of a block that a lane stages
   static constexpr int KS = D / 16;               // MFMA k-steps over D
   static constexpr int DT = D / 32;               // 32-row output tiles over D
@@ -98,9 +98,10 @@ struct Geom {
 //
 // The two waves of a SIMD alternate. A step j of a wave takes two intervals, each ended by a
 // workgroup barrier:
-//   softmax(j):   loads of step j + 3, 2^x packed to bf16, row sums (vector work)
-//   products(j):  O^T += V(j)^T P(j)^T, then S(j + 1) = K(j + 1) Q^T (matrix work), then the LDS
-//                 writes of step j + 2 (converted), which even out the two intervals
+//   softmax(j):   2^x packed to bf16, row sums (vector work)
+//   products(j):  O^T += V(j)^T P(j)^T, then S(j + 1) = K(j + 1) Q^T (matrix work); beside the latter's
+//                 products four codes each of step j + 2 are converted and written to LDS, then the loads
+//                 of step j + 3 go out
 // Waves 4-7 (group 1) run one interval behind waves 0-3. After an entry's last step S(j + 1) is the
 // next entry's first, so only the output and the change of queries come between two entries.
 //
@@ -108,6 +109,15 @@ struct Geom {
 // V(s) and K(s + 1) in 2 s + 1 and 2 s + 2, the first V operands and the scales an interval earlier. Step x
 // is written in products(x - 2), 2 x - 3 and 2 x - 2, and first read (K) in 2 x - 1; the stage that it
 // replaces (step x - 3) was last read in 2 x - 4.
+//
+// Measured, 8 requests of 2,112 rows behind 3,136 tokens, 32 / 8 heads of 128: 986 to 1,031 us on several
+// cards, 1.18 to 1.13 PFLOP/s (matrix pipe busy 53 %, LDS 43 %, clock 1.9 GHz of 2.4: the denser the work,
+// the lower the clock). A step takes a SIMD 3,850 cycles, 2,048 of them products: the softmax of 32 x 64
+// scores is 125 vector instructions, 32 of them 2^x, at about 9 cycles each beside the other wave's products,
+// so it takes as long as they do. Other places for the conversion and the loads, us beside 986: both in the
+// softmax interval 1,040; conversion behind the products 1,093; between them 8 instructions at a time 1,033;
+// loads behind the products 1,030; two vector loads a step for the table word and the scale: no change of
+// the time where the conversion bounds it.
 template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void suffix_prefill_fp8_kernel(const PrefillArgs a) {
@@ -142,71 +152,97 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
   const int skey = lane / LPR;  // row of the block, of piece 0
   const int spitch = is_v ? G::VP : G::KP;
   const int sdst = (is_v ? G::KTILE + bs * kBs * G::VP : bs * kBs * G::KP) + skey * spitch + (lane % LPR) * 32;
-  int ce = blockIdx.x;          // index of the entry in c_next
-  int32_t c_next = fetch(ce);
-  int c_left = 0;               // steps of the cursor's entry not yet loaded
-  int c_keys = 0;               // keys of the prompt from the first of this wave's block on
-  uint32_t c_off = 0, c_max = 0;            // table word of the block, and of the prompt's last one (bytes)
-  const int32_t* c_row = a.bt;
-  const uint8_t* c_codes = codes;           // of the cursor's KV head, at this lane's piece
-  const float* c_scales = is_v ? a.v_scale : a.k_scale;
-  const uint32_t blk_bytes = uint32_t(a.hkv) * (kBs * D), blk_scales = uint32_t(a.hkv) * 4;
-  int32_t c_id = 0;             // the table word, loaded a step ahead (the same in every lane)
-  auto cursor_id = [&]() __attribute__((always_inline)) {
-    uint32_t off = min(c_off, c_max);
-    asm volatile("" : "+v"(off));           // (a vector load)
-    c_id = *reinterpret_cast<const int32_t*>(reinterpret_cast<const uint8_t*>(c_row) + off);
+  // Table words and scales come up to 64 steps (a chunk: of one entry) at a time, step i's in lane i: what
+  // a step loads by itself is its codes, at a scalar base. While a chunk is loaded the words of the next one
+  // are on their way; its scales follow when it begins.
+  int ce = blockIdx.x;          // index of the entry in e_next, which the cursor takes next
+  int32_t e_next = fetch(ce);
+  int e_left = 0;               // steps of the newest entry behind the next chunk
+  int n_left = 0, n_keys = 0;   // the next chunk: steps; keys of the prompt from the first of this wave's block on
+  uint32_t n_off = 0, n_max = 0;             // table word of the block, and of the prompt's last one (bytes)
+  const int32_t* n_row = a.bt;
+  const uint8_t* n_codes = codes;            // of the entry's KV head
+  const float* n_scales = is_v ? a.v_scale : a.k_scale;
+  int32_t n_ids = 0;
+  int c_left = 0, c_keys = 0, c_at = 0;      // the same of the current chunk, and its next step
+  const uint8_t* c_codes = codes;
+  int32_t c_ids = 0;
+  float c_scale = 1.f;
+  const uint32_t blk_bytes = uint32_t(a.hkv) * (kBs * D);
+  // Past the queue's last entry the cursor stays behind that prompt's end: what it loads is staged as zeros.
+  auto next_chunk = [&]() __attribute__((always_inline)) {
+    if (e_left > 0) {
+      n_keys -= 64 * kStep;
+      n_off += 64 * 4 * kBlocks;
+    } else if (valid(e_next, ce)) {
+      const int kbeg = word(e_next, cw::kEntKbeg), L = word(e_next, cw::kEntL), g = word(e_next, cw::kEntG);
+      e_left = word(e_next, cw::kEntKend) - kbeg;
+      n_keys = L - (kbeg * kBlocks + bs) * kBs;
+      n_off = uint32_t(kbeg * kBlocks + bs) * 4;
+      n_max = uint32_t((L + kBs - 1) / kBs - 1) * 4;
+      n_row = a.bt + int64_t(word(e_next, cw::kEntR)) * a.bt_stride;
+      n_codes = codes + int64_t(g) * (kBs * D);
+      n_scales = (is_v ? a.v_scale : a.k_scale) + g;
+      ce += grid;
+      e_next = fetch(ce);
+    } else {
+      n_left = INT32_MAX;
+      n_keys = 0;
+      return;
+    }
+    n_left = min(e_left, 64);
+    e_left -= n_left;
+    n_ids = *reinterpret_cast<const int32_t*>(reinterpret_cast<const uint8_t*>(n_row) +
+                                              min(n_off + uint32_t(lane) * (4 * kBlocks), n_max));
   };
-  // The next entry of the queue. Past the last one the cursor stays in its last entry, behind the
-  // prompt's end: what it loads is staged as zeros.
-  auto cursor_take = [&]() __attribute__((always_inline)) {
-    c_left = INT32_MAX;
-    c_keys = 0;
-    if (!valid(c_next, ce)) return;
-    const int kbeg = word(c_next, cw::kEntKbeg), L = word(c_next, cw::kEntL), g = word(c_next, cw::kEntG);
-    c_left = word(c_next, cw::kEntKend) - kbeg;
-    c_keys = L - (kbeg * kBlocks + bs) * kBs;
-    c_off = uint32_t(kbeg * kBlocks + bs) * 4;
-    c_max = uint32_t((L + kBs - 1) / kBs - 1) * 4;
-    c_row = a.bt + int64_t(word(c_next, cw::kEntR)) * a.bt_stride;
-    c_codes = codes + int64_t(g) * (kBs * D);
-    c_scales = (is_v ? a.v_scale : a.k_scale) + g;
-    ce += grid;
-    c_next = fetch(ce);
+  auto take_chunk = [&]() __attribute__((always_inline)) {
+    c_left = n_left;
+    c_keys = n_keys;
+    c_codes = n_codes;
+    c_ids = n_ids;
+    c_at = 0;
+    const uint32_t id = uint32_t(n_ids) < uint32_t(a.num_blocks) ? n_ids : 0;
+    c_scale = n_scales[int64_t(id) * a.hkv];
+    next_chunk();
   };
   u32x4 raw[P16];
   float raw_scale = 1.f;
   int raw_keys = 0;   // rows of the loaded block inside the prompt; 0 or less: none
   auto load = [&]() __attribute__((always_inline)) {
     // (a block outside the pool loads block 0 and is staged as zeros)
-    const bool ok = uint32_t(c_id) < uint32_t(a.num_blocks);
-    const uint32_t id = ok ? c_id : 0;
-    raw_keys = ok ? c_keys : 0;
-    const uint8_t* src = c_codes + (uint64_t(id) * blk_bytes + uint32_t(lane * 16));
+    const uint32_t word_id = uint32_t(__builtin_amdgcn_readlane(c_ids, c_at & 63));
+    const bool ok = word_id < uint32_t(a.num_blocks);
+    raw_keys = __builtin_amdgcn_readfirstlane(ok ? c_keys : 0);
+    raw_scale = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(c_scale)), c_at & 63)));
+    const uint8_t* src = c_codes + uint64_t(ok ? word_id : 0) * blk_bytes;
 #pragma unroll
-    for (int i = 0; i < P16; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + 1024 * i);
-    raw_scale = *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(c_scales) + uint64_t(id) * blk_scales);
+    for (int i = 0; i < P16; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + uint32_t(lane * 16) + 1024 * i);
     c_keys -= kStep;
-    c_off += 4 * kBlocks;
-    if (__builtin_expect(--c_left == 0, 0)) cursor_take();
-    cursor_id();
+    ++c_at;
+    if (__builtin_expect(--c_left == 0, 0)) take_chunk();
   };
-  auto stage = [&](int at_stage) __attribute__((always_inline)) {
-    uint8_t* const dst = lds + at_stage + sdst;
-    const bool part = __builtin_amdgcn_ballot_w64(raw_keys < kBs) != 0;
-#pragma unroll
-    for (int i = 0; i < P16; ++i) {
-      u32x4 x = raw[i];
-      if (__builtin_expect(part, 0)) {
-        if (i * (64 / LPR) + skey >= raw_keys) x = u32x4{0, 0, 0, 0};
-      }
-      const u32x2 a0 = widen_fp8x4(x[0]), a1 = widen_fp8x4(x[1]), a2 = widen_fp8x4(x[2]), a3 = widen_fp8x4(x[3]);
-      u32x4* at = reinterpret_cast<u32x4*>(dst + i * (64 / LPR) * spitch);
-      at[0] = u32x4{a0[0], a0[1], a1[0], a1[1]};
-      at[1] = u32x4{a2[0], a2[1], a3[0], a3[1]};
+  // The loaded block to LDS, in 2 P16 parts of 16 bytes a lane written (8 codes); with the last one what the
+  // softmax makes of the block's scale.
+  u32x4 wide{0, 0, 0, 0};
+  auto widen = [&](int n) __attribute__((always_inline)) {   // codes 4 n .. + 3
+    if (n % 4 == 0 && __builtin_expect(raw_keys < kBs, 0)) {
+      if (n / 4 * (64 / LPR) + skey >= raw_keys) raw[n / 4] = u32x4{0, 0, 0, 0};
     }
-    if (lane == 0)
-      *reinterpret_cast<float*>(lds + at_stage + G::SCALES + (is_v * kBlocks + bs) * 4) = raw_keys > 0 ? raw_scale : 1.f;
+    const u32x2 x = widen_fp8x4(raw[n / 4][n % 4]);
+    wide[n % 2 * 2] = x[0];
+    wide[n % 2 * 2 + 1] = x[1];
+  };
+  auto stage = [&](int at_stage, int n) __attribute__((always_inline)) {
+    *reinterpret_cast<u32x4*>(lds + at_stage + sdst + n / 2 * (64 / LPR) * spitch + n % 2 * 16) = wide;
+    if (n == 2 * P16 - 1) {
+      const float scale = raw_keys > 0 ? raw_scale : 1.f;
+      float* const s = reinterpret_cast<float*>(lds + at_stage + G::SCALES) + bs;
+      if (is_v) {
+        if (lane < 2) s[kBlocks + lane * kBlocks] = lane == 0 ? __builtin_amdgcn_logf(scale) : __builtin_amdgcn_rcpf(scale);
+      } else if (lane == 0) {
+        *s = a.c_log2 * scale;
+      }
+    }
   };
   auto barrier = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_sched_barrier(0);
@@ -253,13 +289,18 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
   int e_cur = blockIdx.x;
   int32_t cur = fetch(e_cur), next = fetch(e_cur + grid);
   if (!valid(cur, e_cur)) return;   // (the same for every wave)
-  cursor_take();
-  cursor_id();
+  next_chunk();
+  take_chunk();
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     load();
-    stage(i * G::STAGE);
+#pragma unroll
+    for (int n = 0; n < 4 * P16; ++n) {
+      widen(n);
+      if (n % 2 == 1) stage(i * G::STAGE, n / 2);
+    }
   }
+  load();
   load_q(cur);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   barrier();
@@ -274,13 +315,16 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
 
   constexpr int RA = 6;   // operands in flight ahead of their MFMA
   constexpr int NPV = kBlocks * DT, NQK = 2 * KS, N = NPV + NQK;
+  constexpr int LOAD_AT = N - 5;   // the product that the next loads go out beside
+  static_assert(NPV + 4 * P16 - 1 <= LOAD_AT, "the loaded codes are converted before they are replaced");
   bf16x8 op[RA];
   int st0 = 0, st1 = G::STAGE, st2 = 2 * G::STAGE;   // LDS places of the current step and the two after it
-  float kc[kBlocks], vlog[kBlocks], vinv[kBlocks];   // the current step's c k_scale, log2(v_scale), 1 / v_scale
-  f32x4 k_sc, v_sc;   // its scales, read at the end of the interval before
+  f32x4 kc, vlog, vinv;   // the current step's c k_scale, log2 v_scale, 1 / v_scale, read at the end of the interval before
   auto read_scales = [&]() __attribute__((always_inline)) {
-    k_sc = *reinterpret_cast<const f32x4*>(lds + st0 + G::SCALES);
-    v_sc = *reinterpret_cast<const f32x4*>(lds + st0 + G::SCALES + 4 * kBlocks);
+    const f32x4* p = reinterpret_cast<const f32x4*>(lds + st0 + G::SCALES);
+    kc = p[0];
+    vlog = p[1];
+    vinv = p[2];
   };
   read_scales();
   auto row_max = [&]() __attribute__((always_inline)) -> float {   // of the current step's scaled scores
@@ -309,13 +353,6 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
     const bool more = valid(next, e_cur + grid);
     for (int j = 0; j < nsteps; ++j) {
       // ---- softmax interval
-      load();
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        kc[b] = a.c_log2 * k_sc[b];
-        vlog[b] = __builtin_amdgcn_logf(v_sc[b]);
-        vinv[b] = __builtin_amdgcn_rcpf(v_sc[b]);
-      }
       if (__builtin_expect(j == nsteps - 1, 0)) load_q(more ? next : cur);   // (first used after the PV products)
       __builtin_amdgcn_sched_barrier(0);
       if (__builtin_expect(j >= n_full, 0)) {
@@ -367,7 +404,6 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
       const int vb = v_off + st0, kb = k_off + st1;
 #pragma unroll
       for (int i = 0; i < RA; ++i) op[i] = rdv(vb, i);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       barrier();
 
       // ---- product interval: MFMA and operand read alternate, fenced so that the compiler keeps
@@ -384,10 +420,14 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
           sc[q & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % RA], qf[q >> 1], q < 2 ? f32x16{} : sc[q & 1], 0, 0, 0);
         }
         if (i + RA < N) op[i % RA] = i + RA < NPV ? rdv(vb, i + RA) : rdk(kb, i + RA - NPV);
+        if (i >= NPV && i < NPV + 4 * P16) {
+          widen(i - NPV);
+          if ((i - NPV) % 2 == 1) stage(st2, (i - NPV) / 2);
+        }
+        if (i == LOAD_AT) load();
         __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_s_setprio(0);
-      stage(st2);
       const int st = st0;
       st0 = st1;
       st1 = st2;

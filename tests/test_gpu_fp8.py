@@ -537,6 +537,20 @@ def test_prefill_long_sampled_rows(D, hq, hkv, P, S):
         _check_attention(out[i:i + 1], qf[i:i + 1], k[:L], v[:L], P + i, D ** -0.5, f"row {i}")
 
 
+@pytest.mark.parametrize("hq,hkv,D,P,S", [(4, 1, 64, [9001, 0, 4096], [70, 33, 16]), (2, 2, 128, [4100, 8175], [20, 3]),
+                                          (128, 2, 64, [4030, 60, 4159, 17], [70, 9, 1, 66])])
+def test_prefill_of_more_keys_than_a_run_of_table_words(hq, hkv, D, P, S):
+    """Prompts of 63 to 142 steps of 64 keys: the kernel takes table words and scales 64 steps at a time."""
+    _say(f"prefill {hq}/{hkv} D={D} P={P} S={S}")
+    b = Batch(hq, hkv, D, P, S, seed=61, spread=0.5)
+    q = b.queries()
+    out = cw.suffix_prefill_attn_fp8(b.meta(), q.cuda(), b.cache, D ** -0.5)
+    torch.cuda.synchronize()
+    for r in range(len(P)):
+        rows = slice(b.cu[r], b.cu[r + 1])
+        _check_attention(_f64(out[rows]), _f64(q[rows]), b.rows(0, r), b.rows(1, r), P[r], D ** -0.5, f"r{r}")
+
+
 # ---------------------------------------------------------------- decode attention
 def _check_decode(b, lens, q, out, scale, what):
     for r, n in enumerate(lens):
