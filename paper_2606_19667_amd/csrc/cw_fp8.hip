@@ -67,7 +67,8 @@ __device__ __forceinline__ float wave_sum(float x) {
 // TPR threads work on a row (64: a wave, four rows a workgroup; 256: the workgroup), each on
 // CH pieces of 8 columns TPR apart, so that 16 neighbouring lanes hold a group of 128 columns
 // and its maximum takes four exchanges. Sums are fp32.
-// HBM-bound: 7 bytes a column and residual.
+// HBM-bound: 7 bytes a column with a residual. 16,128 rows of 4,096: 80.5 us, 5.8 TB/s (a copy of 1 GiB
+// 5.2); 64 rows 3.8 us in a captured graph, one chain of load, sum, maximum and store.
 // ---------------------------------------------------------------------------
 struct NormArgs {
   const uint16_t* x;
@@ -193,7 +194,10 @@ __global__ __launch_bounds__(kThreads) void add_rms_norm_fp8_kernel(const NormAr
 // 16 (l % 4) .. + 15 of each half of row l / 4 (8 columns at head_dim 64), so a rotary pair
 // lies in one lane, and a block's maximum is a wave reduction. Heads are queries, keys, then
 // values; a wave keeps the cosines and sines of its rows over all its heads.
-// HBM-bound: reads 2 (Hq + 2 Hkv) D bytes a row, writes 2 Hq D + 2 Hkv D.
+// HBM-bound: reads 2 (Hq + 2 Hkv) D bytes a row, writes 2 Hq D + 2 Hkv D. 16,128 rows of 48 heads of 128:
+// 88 us, 4.4 TB/s with the rotation table (a copy of 1 GiB 5.2; what is missing are the ends of the
+// workgroups, each a chain of offsets, table word, rows, maximum, store); 64 requests of one row: 6.9 us in a
+// captured graph, 13.9 called one by one, which is the host's time.
 // ---------------------------------------------------------------------------
 struct AppendArgs {
   const uint16_t* q;
@@ -405,6 +409,10 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp8_kernel(const AppendA
 //    a wave are its own: no barrier in the loop.
 //  * K's scale multiplies the scores and V's the probabilities before they are rounded to
 //    bf16 for the product; sums are fp32.
+// HBM-bound when sequences are long: 64 requests of about 10,367 tokens, 8 KV heads of 128 (1.37 GB) 283 us,
+// 4.85 TB/s (a copy of 1 GiB 5.2). 16 of about 1,407 (46 MB) 16.0 us, 2.9 TB/s: there the chain of length,
+// table word, codes, softmax and the join of the runs bounds it, with two launches. The launch bounds name two
+// waves a SIMD: left to itself the compiler takes fewer registers and the kernel is 25 % slower.
 // ---------------------------------------------------------------------------
 struct DecodeArgs {
   const uint16_t* q;
@@ -717,8 +725,12 @@ extern "C" cw_status cw_add_rms_norm_fp8(const void* x, int64_t x_stride, const 
   a.groups = (hidden + kGroupCols - 1) / kGroupCols;
   a.eps = eps;
   auto* const s = static_cast<hipStream_t>(stream);
+  // A wave per row needs no barrier, a workgroup per row spreads few rows over more waves. us in a captured
+  // graph, 1, 64, 1,000 and 16,000 rows, wave / workgroup: 512 columns 2.76 / 2.79, 3.20 / 3.06, 3.41 / 3.58,
+  // 12.1 / 20.2; 1,024: 3.28 / 2.80, 3.72 / 3.11, 4.26 / 4.04, 19.6 / 24.7 (equal at about 1,600); 2,048:
+  // 4.62 / 3.00, 5.19 / 3.32, 6.06 / 4.84, 37.2 / 36.0; 4,096: 7.27 / 3.53, 8.08 / 3.84, 9.78 / 7.16, 89 / 81.
   if (hidden <= 512) launch_norm<64, 1>(a, s);
-  else if (hidden <= 1024) launch_norm<64, 2>(a, s);
+  else if (hidden <= 1024 && rows > 6 * cw::kNumCu) launch_norm<64, 2>(a, s);
   else if (hidden <= 2048) launch_norm<256, 1>(a, s);
   else if (hidden <= 4096) launch_norm<256, 2>(a, s);
   else if (hidden <= 8192) launch_norm<256, 4>(a, s);

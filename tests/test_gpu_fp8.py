@@ -83,7 +83,7 @@ def _check_norm(x, r, w, eps, out8, scales, h, what):
 
 
 @pytest.mark.parametrize("rows,hidden", [(1, 16), (3, 80), (5, 512), (7, 528), (2, 1024), (9, 1040), (3, 2048), (4, 2064),
-                                         (33, 4096), (5, 4992), (2, 8192), (1, 8208), (3, 16384)])
+                                         (2001, 1024), (1537, 528), (33, 4096), (5, 4992), (2, 8192), (1, 8208), (3, 16384)])
 @pytest.mark.parametrize("residual", [True, False])
 def test_norm(rows, hidden, residual):
     _say(f"norm {rows} x {hidden} residual={residual}")
