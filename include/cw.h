@@ -620,7 +620,9 @@ cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const void* k, int
  *   plan_host / plan_dev   the unsplit plan of cw_suffix_prefill_plan
  * A table entry outside [0, num_blocks) is read as zero keys and values, each
  * with score 0. A NaN code of a visible key or value makes the outputs that see
- * it NaN; codes behind a prompt's end are never used.
+ * it NaN, and a NaN value code of a suffix row also those of earlier rows of the
+ * request that stand in the same 64 tokens; codes behind a prompt's end are never
+ * used.
  * Errors as cw_suffix_prefill_attn (P_r need not be a multiple of 16), plus
  * CW_EINVAL for a misaligned pointer. */
 cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, const void* v8, const float* k_scale,
@@ -629,6 +631,26 @@ cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, const void* 
                                      int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                      int32_t block_size, int32_t num_blocks, float softmax_scale,
                                      const int32_t* plan_host, const int32_t* plan_dev, void* out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: cw_suffix_prefill_attn_fp8 with each tile's keys in runs, for few
+ * suffix rows behind long prefixes (a question after cached evidence), as
+ * cw_suffix_prefill_attn_split is of cw_suffix_prefill_attn: a plan of
+ * cw_suffix_prefill_plan with num_splits runs; the runs' parts are combined as
+ * by cw_lse_merge.
+ *   workspace   device, 16-byte aligned, at least
+ *               cw_suffix_prefill_split_workspace_bytes(total_s, Hq, D, num_splits)
+ *               bytes; overwritten. Calls that may run at the same time need
+ *               workspaces of their own.
+ * Errors as cw_suffix_prefill_attn_fp8, plus CW_EINVAL for a missing, too small
+ * or misaligned workspace. */
+cw_status cw_suffix_prefill_attn_split_fp8(const void* q, const void* k8, const void* v8, const float* k_scale,
+                                           const float* v_scale, const int32_t* block_table, int32_t bt_stride,
+                                           const int32_t* cu_suffix_host, const int32_t* prefix_len_host,
+                                           int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                           int32_t head_dim, int32_t block_size, int32_t num_blocks,
+                                           float softmax_scale, const int32_t* plan_host, const int32_t* plan_dev,
+                                           void* workspace, int64_t workspace_bytes, void* out, void* stream);
 
 /* ------------------------------------------------------------------------
  * Device: attention of one query row per request over the 8-bit cache (the next

@@ -59,6 +59,9 @@ struct PrefillArgs {
   const int32_t* bt;
   const int32_t* plan;   // device copy of the whole plan (header, then entries)
   uint16_t* out;
+  float* part_o;         // split plans: fp32 [splits][part_rows][D], normalised
+  float* part_lse;       // and base-2 log-sum-exp [splits][part_rows]
+  int64_t part_rows;     // total suffix rows * hq
   int32_t bt_stride, hq, hkv, group, per_tile, num_blocks, num_entries;
   float c_log2;
   uint32_t fp_lo, fp_hi; // the batch fingerprint the host validated
@@ -118,7 +121,9 @@ struct Geom {
 // softmax interval 1,040; conversion behind the products 1,093; between them 8 instructions at a time 1,033;
 // loads behind the products 1,030; two vector loads a step for the table word and the scale: no change of
 // the time where the conversion bounds it.
-template <int D>
+// SPLIT: the entries are runs of a tile's keys (a plan of several runs), and each writes its part, zeros and
+// -inf for rows that see none of the run's keys. A run of no steps goes through one that no row sees.
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void suffix_prefill_fp8_kernel(const PrefillArgs a) {
   using G = Geom<D>;
@@ -178,6 +183,10 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
       const int kbeg = word(e_next, cw::kEntKbeg), L = word(e_next, cw::kEntL), g = word(e_next, cw::kEntG);
       e_left = word(e_next, cw::kEntKend) - kbeg;
       n_keys = L - (kbeg * kBlocks + bs) * kBs;
+      if (SPLIT && e_left == 0) {   // a run of no steps: one of zeros
+        e_left = 1;
+        n_keys = 0;
+      }
       n_off = uint32_t(kbeg * kBlocks + bs) * 4;
       n_max = uint32_t((L + kBs - 1) / kBs - 1) * 4;
       n_row = a.bt + int64_t(word(e_next, cw::kEntR)) * a.bt_stride;
@@ -346,10 +355,12 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
   barrier();
 
   for (;;) {
-    const int kbeg = word(cur, cw::kEntKbeg), nsteps = word(cur, cw::kEntKend) - kbeg;
+    const int kbeg = word(cur, cw::kEntKbeg), keysteps = word(cur, cw::kEntKend) - kbeg;
+    const int nsteps = SPLIT ? max(keysteps, 1) : keysteps;
     const int n_full = word(cur, cw::kEntNfull), nvalid = word(cur, cw::kEntNvalid);
     const int g = word(cur, cw::kEntG), qrow0 = word(cur, cw::kEntQrow);
-    const int qpos = word(cur, cw::kEntP) + word(cur, cw::kEntRow0) + pos;   // keys 0 .. qpos are visible
+    // keys 0 .. qpos are visible (none in a run of no steps, which goes through one)
+    const int qpos = SPLIT && keysteps == 0 ? -1 : word(cur, cw::kEntP) + word(cur, cw::kEntRow0) + pos;
     const bool more = valid(next, e_cur + grid);
     for (int j = 0; j < nsteps; ++j) {
       // ---- softmax interval
@@ -440,30 +451,47 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
     // ---- the entry's end (part of the next softmax interval): 64 columns at a time through the
     // wave's own area, so that whole lines are stored
     const float total = sum_pair32(l);
-    const float inv = has_row(cur) ? 1.f / total : 0.f;
-    uint8_t* const stg = lds + RING * G::STAGE + wave * G::OUT;
-    constexpr int OP = 64 * 2 + 16;
+    if constexpr (SPLIT) {
+      // (a row that sees none of the run's keys has the sum +0. Tests of the bits: a NaN has to pass, and its part
+      // has to count in the merge, which takes a NaN log-sum-exp for an empty part: a large number stands there.)
+      const bool any = __float_as_uint(total) != 0, bad = (__float_as_uint(total) & 0x7FFFFFFFu) > 0x7F800000u;
+      const float inv = any ? 1.f / total : 0.f;
+      if (has_row(cur)) {
+        const int64_t at = int64_t(word(cur, cw::kEntSplit)) * a.part_rows + (int64_t(qrow0) + pos) * a.hq + g * a.group + hh;
 #pragma unroll
-    for (int rd = 0; rd < D / 64; ++rd) {
-      asm volatile("" ::: "memory");
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+          for (int gq = 0; gq < 4; ++gq)
+            *reinterpret_cast<f32x4*>(a.part_o + at * D + 32 * t + 8 * gq + 4 * half) =
+                f32x4{oacc[t][4 * gq] * inv, oacc[t][4 * gq + 1] * inv, oacc[t][4 * gq + 2] * inv, oacc[t][4 * gq + 3] * inv};
+        if (half == 0) a.part_lse[at] = bad ? 1e30f : any ? m + __builtin_amdgcn_logf(total) : -INFINITY;
+      }
+    } else {
+      const float inv = has_row(cur) ? 1.f / total : 0.f;
+      uint8_t* const stg = lds + RING * G::STAGE + wave * G::OUT;
+      constexpr int OP = 64 * 2 + 16;
 #pragma unroll
-        for (int gq = 0; gq < 4; ++gq) {
-          const f32x16& o = oacc[2 * rd + t];   // rows 8 gq + 4 half .. + 3: columns of the output
-          *reinterpret_cast<u32x2*>(stg + l32 * OP + t * 64 + gq * 16 + half * 8) =
-              u32x2{pack_bf16x2(o[4 * gq] * inv, o[4 * gq + 1] * inv),
-                    pack_bf16x2(o[4 * gq + 2] * inv, o[4 * gq + 3] * inv)};
+      for (int rd = 0; rd < D / 64; ++rd) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int gq = 0; gq < 4; ++gq) {
+            const f32x16& o = oacc[2 * rd + t];   // rows 8 gq + 4 half .. + 3: columns of the output
+            *reinterpret_cast<u32x2*>(stg + l32 * OP + t * 64 + gq * 16 + half * 8) =
+                u32x2{pack_bf16x2(o[4 * gq] * inv, o[4 * gq + 1] * inv),
+                      pack_bf16x2(o[4 * gq + 2] * inv, o[4 * gq + 3] * inv)};
+          }
+        asm volatile("" ::: "memory");   // (lanes read what other lanes of the wave wrote, in order)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int rr = i * 8 + lane / 8, mr = wave * 32 + rr;
+          const int hr = mr / a.per_tile, pr = mr - hr * a.per_tile;
+          const u32x4 x = *reinterpret_cast<const u32x4*>(stg + rr * OP + (lane & 7) * 16);
+          if (hr < a.group && pr < nvalid)
+            *reinterpret_cast<u32x4*>(a.out + ((int64_t(qrow0) + pr) * a.hq + g * a.group + hr) * D + rd * 64 +
+                                      (lane & 7) * 8) = x;
         }
-      asm volatile("" ::: "memory");   // (lanes read what other lanes of the wave wrote, in order)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int rr = i * 8 + lane / 8, mr = wave * 32 + rr;
-        const int hr = mr / a.per_tile, pr = mr - hr * a.per_tile;
-        const u32x4 x = *reinterpret_cast<const u32x4*>(stg + rr * OP + (lane & 7) * 16);
-        if (hr < a.group && pr < nvalid)
-          *reinterpret_cast<u32x4*>(a.out + ((int64_t(qrow0) + pr) * a.hq + g * a.group + hr) * D + rd * 64 +
-                                    (lane & 7) * 8) = x;
       }
     }
     if (!more) break;
@@ -477,17 +505,15 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
   if (!group1) barrier();
 }
 
-}  // namespace
-
-extern "C" cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, const void* v8, const float* k_scale,
-                                                const float* v_scale, const int32_t* block_table, int32_t bt_stride,
-                                                const int32_t* cu_suffix_host, const int32_t* prefix_len_host,
-                                                int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
-                                                int32_t head_dim, int32_t block_size, int32_t num_blocks,
-                                                float softmax_scale, const int32_t* plan_host,
-                                                const int32_t* plan_dev, void* out, void* stream) {
-  const std::string w("suffix_prefill_attn_fp8");
-  cw_status st = cw::check_cache_fp8(w.c_str(), k8, v8, k_scale, v_scale, block_table, num_kv_heads, head_dim,
+// Checks and launch of both entry points; workspace NULL: of a plan without splits.
+cw_status prefill_fp8(const char* what, const void* q, const void* k8, const void* v8, const float* k_scale,
+                      const float* v_scale, const int32_t* block_table, int32_t bt_stride,
+                      const int32_t* cu_suffix_host, const int32_t* prefix_len_host, int32_t batch,
+                      int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                      int32_t num_blocks, float softmax_scale, const int32_t* plan_host, const int32_t* plan_dev,
+                      bool split, void* workspace, int64_t workspace_bytes, void* out, void* stream) {
+  const std::string w(what);
+  cw_status st = cw::check_cache_fp8(what, k8, v8, k_scale, v_scale, block_table, num_kv_heads, head_dim,
                                      block_size, num_blocks);
   if (st != CW_OK) return st;
   if (num_q_heads < 1 || num_q_heads % num_kv_heads != 0)
@@ -501,10 +527,17 @@ extern "C" cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, c
   if (st != CW_OK) return st;
   PrefillArgs a;
   int32_t grid = 0, splits = 1;
-  st = cw::check_plan_header("suffix_prefill_attn_fp8", plan_host, cu_suffix_host, prefix_len_host, batch, num_q_heads,
-                             num_kv_heads, head_dim, &grid, &splits, &a.fp_lo, &a.fp_hi, &a.num_entries);
+  st = cw::check_plan_header(what, plan_host, cu_suffix_host, prefix_len_host, batch, num_q_heads, num_kv_heads,
+                             head_dim, &grid, &splits, &a.fp_lo, &a.fp_hi, &a.num_entries);
   if (st != CW_OK) return st;
-  if (splits != 1) return cw::fail(CW_EINVAL, w + ": the plan has splits");
+  if (!split && splits != 1) return cw::fail(CW_EINVAL, w + ": the plan has splits");
+  a.part_rows = rows * num_q_heads;
+  if (split) {
+    const int64_t need = cw_suffix_prefill_split_workspace_bytes(rows, num_q_heads, head_dim, splits);
+    if (need < 0) return cw_status(need);
+    if (rows > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15) != 0))
+      return cw::fail(CW_EINVAL, w + ": workspace must hold " + std::to_string(need) + " bytes, 16-byte aligned");
+  }
   if (rows == 0 || grid == 0) return cw::ok();
   if (!q || !out || !plan_dev) return cw::fail(CW_EINVAL, w + ": a required pointer is NULL");
   if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15) != 0)
@@ -517,6 +550,11 @@ extern "C" cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, c
   a.bt = block_table;
   a.plan = plan_dev;
   a.out = static_cast<uint16_t*>(out);
+  a.part_o = static_cast<float*>(workspace);
+  // (the layout that cw_suffix_prefill_split_workspace_bytes counts: parts, then sums at a multiple of 256)
+  a.part_lse = split ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
+                                                (int64_t(splits) * a.part_rows * head_dim * 4 + 255) / 256 * 256)
+                     : nullptr;
   a.bt_stride = bt_stride;
   a.hq = num_q_heads;
   a.hkv = num_kv_heads;
@@ -525,11 +563,36 @@ extern "C" cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, c
   a.num_blocks = num_blocks;
   a.c_log2 = softmax_scale * 1.4426950408889634f;
   auto* const s = static_cast<hipStream_t>(stream);
-  if (head_dim == 128)
-    hipLaunchKernelGGL(suffix_prefill_fp8_kernel<128>, dim3(unsigned(grid)), dim3(kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL(suffix_prefill_fp8_kernel<64>, dim3(unsigned(grid)), dim3(kThreads), 0, s, a);
+  auto* const kernel = head_dim == 128 ? (split ? suffix_prefill_fp8_kernel<128, true> : suffix_prefill_fp8_kernel<128, false>)
+                                       : (split ? suffix_prefill_fp8_kernel<64, true> : suffix_prefill_fp8_kernel<64, false>);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(kThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return cw::fail(CW_EHIP, w + " launch: " + hipGetErrorString(e));
-  return cw::ok();
+  if (!split) return cw::ok();
+  return cw_lse_merge(a.part_o, a.part_lse, splits, a.part_rows, head_dim, out, stream);
+}
+
+}  // namespace
+
+extern "C" cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, const void* v8, const float* k_scale,
+                                                const float* v_scale, const int32_t* block_table, int32_t bt_stride,
+                                                const int32_t* cu_suffix_host, const int32_t* prefix_len_host,
+                                                int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                                int32_t head_dim, int32_t block_size, int32_t num_blocks,
+                                                float softmax_scale, const int32_t* plan_host,
+                                                const int32_t* plan_dev, void* out, void* stream) {
+  return prefill_fp8("suffix_prefill_attn_fp8", q, k8, v8, k_scale, v_scale, block_table, bt_stride, cu_suffix_host,
+                     prefix_len_host, batch, num_q_heads, num_kv_heads, head_dim, block_size, num_blocks,
+                     softmax_scale, plan_host, plan_dev, false, nullptr, 0, out, stream);
+}
+
+extern "C" cw_status cw_suffix_prefill_attn_split_fp8(
+    const void* q, const void* k8, const void* v8, const float* k_scale, const float* v_scale,
+    const int32_t* block_table, int32_t bt_stride, const int32_t* cu_suffix_host, const int32_t* prefix_len_host,
+    int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+    int32_t num_blocks, float softmax_scale, const int32_t* plan_host, const int32_t* plan_dev, void* workspace,
+    int64_t workspace_bytes, void* out, void* stream) {
+  return prefill_fp8("suffix_prefill_attn_split_fp8", q, k8, v8, k_scale, v_scale, block_table, bt_stride,
+                     cu_suffix_host, prefix_len_host, batch, num_q_heads, num_kv_heads, head_dim, block_size,
+                     num_blocks, softmax_scale, plan_host, plan_dev, true, workspace, workspace_bytes, out, stream);
 }

@@ -104,6 +104,8 @@ def _load() -> ctypes.CDLL:
                                       _i32, _vp, _vp, _pi32, _pi32, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
         "cw_suffix_prefill_attn_fp8": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _pi32, _pi32, _i32, _i32, _i32,
                                               _i32, _i32, _i32, _f32, _pi32, _vp, _vp, _vp]),
+        "cw_suffix_prefill_attn_split_fp8": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _pi32, _pi32, _i32, _i32, _i32,
+                                                    _i32, _i32, _i32, _f32, _pi32, _vp, _vp, _i64, _vp, _vp]),
         "cw_decode_attn_fp8_workspace_bytes": (_i64, [_i32, _i32, _i32, _i32]),
         "cw_decode_attn_fp8": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
                                       _f32, _i32, _vp, _i64, _vp, _vp]),
@@ -130,6 +132,7 @@ EXPORTED = ("cw_abi_version", "cw_last_error", "cw_block_hashes", "cw_pool_creat
             "cw_tree_create", "cw_tree_destroy", "cw_tree_num_nodes", "cw_tree_insert",
             "cw_tree_mark_stale", "cw_tree_order", "cw_rope_table", "cw_qkv_rope_append",
             "cw_add_rms_norm_fp8", "cw_fp8_linear", "cw_rope_append_fp8", "cw_suffix_prefill_attn_fp8",
+            "cw_suffix_prefill_attn_split_fp8",
             "cw_decode_attn_fp8_workspace_bytes", "cw_decode_attn_fp8",
             "cw_probe_mfma_bf16_flops", "cw_probe_mfma_bf16")
 
@@ -955,6 +958,51 @@ def suffix_prefill_attn_fp8(meta: BatchMeta, q: torch.Tensor, cache: Fp8KvCache,
         _arg(q, bf16, "q", dev), *cache._args(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
         meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.k.shape[0],
         softmax_scale, meta._hp(meta.plan_host), _arg(meta.plan, i32, "plan", dev), _arg(out, bf16, "out", dev),
+        _stream_of(stream, dev)))
+    return out
+
+
+def split_count_fp8(meta: BatchMeta) -> int:
+    """A split count for cw_suffix_prefill_attn_split_fp8: split_count's, with runs of 512
+    keys at least. Measured, us (32 / 8 heads of 128; unsplit, then by runs): 4 x 48 rows behind
+    10,000 tokens 227; 4, 8, 16 runs 72, 55, 64. 1 x 48 behind 10,000 223; 8, 16, 32 runs 44, 36,
+    37. 1 x 64 behind 5,000 116; 8, 16, 32 runs 31, 32, 35. 8 x 64 behind 2,000 55; 2, 4, 8 runs
+    42, 36, 48. 4 x 64 behind 700 25; 2, 4, 8 runs 24, 25, 29."""
+    longest = int((meta.plen_host + np.diff(meta.cu_host)).max())
+    return max(1, min(split_count(meta), longest // 512))
+
+
+def suffix_prefill_attn_split_fp8(meta: BatchMeta, q: torch.Tensor, cache: Fp8KvCache, softmax_scale: float,
+                                  num_splits: int | None = None, workspace: torch.Tensor | None = None,
+                                  out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """cw_suffix_prefill_attn_split_fp8: suffix_prefill_attn_fp8 with each tile's keys in
+    num_splits runs (by default split_count_fp8's; without runs the call is
+    suffix_prefill_attn_fp8), for few rows behind long prefixes.
+    `workspace` (uint8, device) is allocated when not given; calls that may run
+    at the same time, captured ones among them, need one each."""
+    if DEBUG_CHECK_COPIES:
+        meta.check_device_copies()
+    hq, hkv, D = meta.num_q_heads, meta.num_kv_heads, meta.head_dim
+    if q.shape != (meta.total_rows, hq, D):
+        raise ValueError(f"q must be [{meta.total_rows}, {hq}, {D}], got {tuple(q.shape)}")
+    if out is None:
+        out = _new(stream, q.shape, torch.bfloat16, q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if num_splits is None:
+        num_splits = split_count_fp8(meta)
+        if num_splits == 1:
+            return suffix_prefill_attn_fp8(meta, q, cache, softmax_scale, out, stream)
+    need = split_workspace_bytes(meta, num_splits)
+    if workspace is None:
+        workspace = _new(stream, max(need, 1), torch.uint8, q.device)
+    plan_host, plan_dev = meta.split_plan(int(num_splits))
+    dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
+    _check(_lib.cw_suffix_prefill_attn_split_fp8(
+        _arg(q, bf16, "q", dev), *cache._args(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
+        meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.k.shape[0],
+        softmax_scale, meta._hp(plan_host), _arg(plan_dev, i32, "plan", dev),
+        _arg(workspace, torch.uint8, "workspace", dev), workspace.numel(), _arg(out, bf16, "out", dev),
         _stream_of(stream, dev)))
     return out
 

@@ -187,6 +187,26 @@ def test_prefill_refusals(status, change):
     assert cw.last_error()
 
 
+def _split(ws=d_, wb=1 << 20, splits=2, **kw):
+    plan = cw.suffix_prefill_plan(i32(0, 3, 5), i32(7, 20), 8, 2, 64, splits)
+    a = dict(q=d_, k8=d_, v8=d_, sk=d_, sv=d_, bt=d_, stride=4, cu=i32(0, 3, 5), pl=i32(7, 20), batch=2, hq=8, hkv=2, d=64,
+             bs=16, nb=9, scale=0.1, plan_dev=d_, out=d_)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return cw.lib().cw_suffix_prefill_attn_split_fp8(
+        a["q"], a["k8"], a["v8"], a["sk"], a["sv"], a["bt"], a["stride"], p32(a["cu"]), p32(a["pl"]), a["batch"], a["hq"],
+        a["hkv"], a["d"], a["bs"], a["nb"], a["scale"], p32(plan), a["plan_dev"], ws, wb, a["out"], None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (E, dict(ws=None)), (E, dict(ws=odd)), (E, dict(wb=2 * 40 * 65 * 4 - 1)), (E, dict(q=None)), (E, dict(out=None)),
+    (E, dict(plan_dev=None)), (E, dict(pl=i32(8, 20))), (E, dict(hq=16)), (E, dict(scale=-1.0)), (U, dict(d=96)),
+])
+def test_split_prefill_refusals(status, change):
+    assert _split(**change) == status
+    assert "suffix_prefill_attn_split_fp8" in cw.last_error()
+
+
 def _decode(q=d_, k8=d_, v8=d_, sk=d_, sv=d_, bt=d_, stride=4, lens=d_, batch=2, hq=8, hkv=2, d=64, bs=16, nb=9, scale=0.1,
             splits=1, ws=None, wb=0, out=d_):
     return cw.lib().cw_decode_attn_fp8(q, k8, v8, sk, sv, bt, stride, lens, batch, hq, hkv, d, bs, nb, scale, splits, ws,
@@ -216,6 +236,14 @@ def test_decode_workspace_and_split_count():
     for b, hq, hkv, n in ((1, 32, 8, 1), (1, 32, 8, 200), (16, 32, 8, 1408), (64, 64, 8, 10368), (1, 4, 1, 10 ** 6)):
         s = cw.decode_split_count(b, hq, hkv, n)
         assert 1 <= s <= 64 and (s == 1 or n // s >= 256)
+
+
+def test_split_count_keeps_runs_of_512_keys():
+    for P, S, most in (([10000], [48], 19), ([700, 3], [64, 1], 1), ([0], [1], 1), ([5000, 5000], [64, 64], 9)):
+        cu = np.concatenate([[0], np.cumsum(S)])
+        meta = cw.BatchMeta(np.zeros((len(P), 700)), cu, P, 32, 8, 128, device=None)
+        n = cw.split_count_fp8(meta)
+        assert 1 <= n <= most and n <= cw.split_count(meta)
 
 
 def test_python_argument_checks():

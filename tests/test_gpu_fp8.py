@@ -551,6 +551,63 @@ def test_prefill_of_more_keys_than_a_run_of_table_words(hq, hkv, D, P, S):
         _check_attention(_f64(out[rows]), _f64(q[rows]), b.rows(0, r), b.rows(1, r), P[r], D ** -0.5, f"r{r}")
 
 
+SPLIT_CASES = [
+    (8, 2, 128, [1000, 0, 63], [17, 5, 1]),
+    (28, 4, 128, [700, 40], [40, 3]),
+    (4, 1, 64, [5000, 3, 4100], [9, 70, 64]),
+    (128, 2, 64, [130], [5]),
+]
+
+
+@pytest.mark.parametrize("hq,hkv,D,P,S", SPLIT_CASES)
+@pytest.mark.parametrize("splits", [None, 1, 2, 7, 64])
+def test_prefill_split(hq, hkv, D, P, S, splits):
+    """Runs of keys, some of them empty (short prompts) or unseen by some rows, joined."""
+    _say(f"split prefill {hq}/{hkv} D={D} P={P} S={S} x{splits}")
+    b = Batch(hq, hkv, D, P, S, seed=71 + hq, spread=0.5)
+    q, meta = b.queries(), b.meta()
+    n = cw.split_count_fp8(meta) if splits is None else splits
+    ws = torch.full((cw.split_workspace_bytes(meta, n) + 64,), 0xFF, dtype=torch.uint8, device="cuda")   # NaN
+    out = torch.full((b.T + 3, hq, D), 9.0, dtype=torch.bfloat16, device="cuda")
+    cw.suffix_prefill_attn_split_fp8(meta, q.cuda(), b.cache, D ** -0.5, num_splits=splits, workspace=ws, out=out[:b.T])
+    torch.cuda.synchronize()
+    assert (out[b.T:] == 9).all() and (ws[-64:] == 0xFF).all()
+    for r in range(len(P)):
+        rows = slice(b.cu[r], b.cu[r + 1])
+        _check_attention(_f64(out[rows]), _f64(q[rows]), b.rows(0, r), b.rows(1, r), P[r], D ** -0.5, f"r{r}")
+
+
+def test_prefill_split_nan_and_capture():
+    """A NaN key code reaches the rows that see it, whichever run holds it; two captured calls with workspaces
+    that they allocate themselves, replayed with other queries between eager calls, have the eager bits."""
+    b = Batch(4, 1, 64, [600], [40], seed=72, spread=0.0)
+    b.codes[0][b.bt[0, 38], 0, 7, 7] = NAN8      # key 615
+    cache = cw.Fp8KvCache.of(b.codes[0].cuda().view(cw.FP8), b.cache.v, b.cache.k_scale, b.cache.v_scale)
+    out = _f64(cw.suffix_prefill_attn_split_fp8(b.meta(), b.queries().cuda(), cache, 0.125, num_splits=4))
+    assert np.isfinite(out[:15]).all() and np.isnan(out[15:]).all()
+    meta = b.meta()
+    sets = []
+    for n in (3, 5):
+        meta.split_plan(n)   # (its copy to the device is not for a graph)
+        q = torch.zeros(40, 4, 64, dtype=torch.bfloat16, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            got = cw.suffix_prefill_attn_split_fp8(meta, q, b.cache, 0.125, num_splits=n)
+        sets.append((n, q, graph, got))
+    for step in range(4):
+        want = []
+        for n, q, _, _ in sets:
+            q.copy_(b.queries().cuda())
+            want.append(cw.suffix_prefill_attn_split_fp8(meta, q, b.cache, 0.125, num_splits=n))
+        torch.cuda.synchronize()
+        for s in sets:
+            s[2].replay()
+        torch.cuda.synchronize()
+        for s, w in zip(sets, want):
+            assert torch.equal(_bits(s[3]), _bits(w)), step
+
+
 # ---------------------------------------------------------------- decode attention
 def _check_decode(b, lens, q, out, scale, what):
     for r, n in enumerate(lens):
