@@ -673,6 +673,24 @@ def test_decode_lengths_out_of_range_and_foreign_blocks(splits):
     _check_decode(b, lens, q, out, 0.125, "out of range")
 
 
+@pytest.mark.parametrize("splits", [1, 4])
+@pytest.mark.parametrize("key,sees", [(0, True), (299, True), (300, False)])
+def test_decode_nan_codes(splits, key, sees):
+    """A NaN key code makes its KV head's outputs NaN, a NaN value code its column; behind the length neither does."""
+    b = Batch(8, 2, 64, [320, 40], [0, 0], seed=24, spread=0.0)
+    q, lens = b.queries(2).cuda(), torch.tensor([300, 40], dtype=torch.int32).cuda()
+    bt = torch.from_numpy(b.bt).cuda()
+    for which in (0, 1):
+        codes = [c.clone() for c in b.codes]
+        codes[which][b.bt[0, key // BS], 1, key % BS, 9] = NAN8
+        cache = cw.Fp8KvCache.of(*(c.cuda().view(cw.FP8) for c in codes), b.cache.k_scale, b.cache.v_scale)
+        out = _f64(cw.decode_attn_fp8(q, cache, bt, lens, 0.125, num_splits=splits))
+        bad = np.zeros(out.shape, bool)
+        if sees:
+            bad[0, 4:, slice(None) if which == 0 else 9] = True
+        assert np.array_equal(np.isnan(out), bad), which
+
+
 def test_decode_captured_replays_follow_growing_lengths():
     """Two captured decode calls with workspaces of their own, replayed in turn with other lengths
     and queries, equal eager calls each time."""
