@@ -384,7 +384,7 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
         m = mx == -INFINITY ? 0.f : mx;
       }
       float l_new;
-      for (;;) {
+      for (bool moved = false;; moved = true) {
         l_new = l;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
@@ -400,11 +400,12 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
           l_new = fmaf(sum, vinv[b], l_new);
         }
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(l_new > kMaxSum) == 0, 1)) break;
-        // (a second pass at most brings every row of the step to its own maximum: with l at 2^30
-        // or below and probabilities up to 1 the sum is in range again, so the loop ends)
+        // Two passes at most: the second has every row that moved at its own maximum, with l at 1 or below and
+        // probabilities up to 1, so its sum is in range again. What is not by then (NaN, value scales near
+        // fp32's end) stays as it is. (The exit stands behind `to`: ahead of it the registers spill.)
         const float before = max_pair32(l), top = max_pair32(l_new);   // (both halves hold the same row)
         const float to = top > kMaxSum ? fmaxf(row_max(), before > 1.f ? m + __builtin_amdgcn_logf(before) : m) : m;
-        if (__builtin_amdgcn_ballot_w64(to != m) == 0) break;   // (nothing to move: values that are no numbers)
+        if (moved) break;
         const float alpha = __builtin_amdgcn_exp2f(m - to);
         l *= alpha;
 #pragma unroll

@@ -608,6 +608,24 @@ def test_prefill_split_nan_and_capture():
             assert torch.equal(_bits(s[3]), _bits(w)), step
 
 
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prefill_ends_beside_values_out_of_range(D, splits):
+    """One head's value scales are 2^126, so its rows' sums leave fp32 and its outputs are no numbers; one of
+    its query rows is NaN. The call ends, the NaN row is NaN, and the other head's rows are right."""
+    _say(f"out of range D={D} splits={splits}")
+    b = Batch(8, 2, D, [70], [40], seed=81, spread=0.0)
+    b.scale[1][:, 1] = 2.0 ** 126
+    cache = cw.Fp8KvCache.of(b.cache.k, b.cache.v, b.cache.k_scale, b.scale[1].cuda())
+    q = b.queries()
+    q[3, 4:] = float("nan")
+    meta, qd = b.meta(), q.cuda()
+    got = _f64(cw.suffix_prefill_attn_fp8(meta, qd, cache, D ** -0.5) if splits == 1 else
+               cw.suffix_prefill_attn_split_fp8(meta, qd, cache, D ** -0.5, num_splits=splits))
+    assert np.isnan(got[3, 4:]).all()
+    _check_attention(got[:, :4], _f64(q[:, :4]), b.rows(0, 0)[:, :1], b.rows(1, 0)[:, :1], 70, D ** -0.5, f"D={D}")
+
+
 # ---------------------------------------------------------------- decode attention
 def _check_decode(b, lens, q, out, scale, what):
     for r, n in enumerate(lens):
