@@ -35,8 +35,9 @@ HIP_SOURCES = ["cw_kernels.hip", "cw_qkv.hip", "cw_probe.hip", "cw_fp8.hip", "cw
 HIP_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
     "-mcode-object-version=5",
-    # no NaN operands reach the kernels' float code (masked scores are -inf,
-    # never NaN), which lets max reductions use v_max3 without quieting
+    # the bf16 kernels make no NaN themselves (masked scores are -inf) and promise
+    # nothing for NaN inputs, which lets max reductions use v_max3 without quieting;
+    # the 8-bit calls do say where NaN goes (below)
     "-fno-honor-nans",
     # keep the compiler from forming packed fp32 VALU instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -46,10 +47,14 @@ HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra"]
 # Per-source extra flags. The attention kernel's step has uniform (wave-wide)
 # branches only; structurizing them makes the register allocator keep two
 # copies of the 64-register output accumulator across the branch arms, which
-# overflows the 256-register budget of two waves per SIMD. The norm and the
-# append of the 8-bit path tell NaN and infinite values apart.
+# overflows the 256-register budget of two waves per SIMD. The calls of the
+# 8-bit path promise where NaN codes and values go, so comparisons with NaN have
+# to mean what they say there (the product's code is the same either way, the
+# prefill takes the same time). Runs of keys are joined by cw_kernels.hip, which
+# only multiplies and adds their values: a NaN log-sum-exp does not get there.
 EXTRA_FLAGS = {"cw_kernels.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"],
-               "cw_fp8_prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"],
+               "cw_fp8_prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true", "-fhonor-nans"],
+               "cw_fp8_linear.hip": ["-fhonor-nans"],
                "cw_fp8.hip": ["-fhonor-nans"]}
 
 

@@ -280,3 +280,12 @@ def test_python_argument_checks():
     with pytest.raises(TypeError, match="k must be a torch tensor"):
         cw._rows(None, torch.bfloat16, "k", 0)
 
+
+def test_8_bit_sources_are_built_with_nan_honoured():
+    """The header says where NaN codes go; the build's default lets the compiler assume that there are none."""
+    from paper_2606_19667_amd import build
+    sources = [s for s in build.HIP_SOURCES if "fp8" in s]
+    assert len(sources) == 3
+    for s in sources:
+        honor = [f for f in build.HIP_FLAGS + build.EXTRA_FLAGS.get(s, []) if f.endswith("honor-nans")]
+        assert honor[-1] == "-fhonor-nans", s
