@@ -619,10 +619,11 @@ cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const void* k, int
  * probabilities' sum: values above 2^96 in magnitude may overflow them.
  *   plan_host / plan_dev   the unsplit plan of cw_suffix_prefill_plan
  * A table entry outside [0, num_blocks) is read as zero keys and values, each
- * with score 0. A NaN code of a visible key or value makes the outputs that see
- * it NaN, and a NaN value code of a suffix row also those of earlier rows of the
- * request that stand in the same 64 tokens; codes behind a prompt's end are never
- * used.
+ * with score 0. A NaN key code makes all outputs of its KV head's query heads NaN
+ * in the rows that see it, and no others; a NaN value code its column of them. A NaN
+ * value code of a suffix row can also reach (0 times NaN in the matrix product) the
+ * same column in earlier rows of the request, those at most 256 / (Hq / Hkv) + 62
+ * tokens before it. Codes behind a prompt's end are never used.
  * Errors as cw_suffix_prefill_attn (P_r need not be a multiple of 16), plus
  * CW_EINVAL for a misaligned pointer. */
 cw_status cw_suffix_prefill_attn_fp8(const void* q, const void* k8, const void* v8, const float* k_scale,

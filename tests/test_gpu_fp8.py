@@ -626,6 +626,33 @@ def test_prefill_ends_beside_values_out_of_range(D, splits):
     _check_attention(got[:, :4], _f64(q[:, :4]), b.rows(0, 0)[:, :1], b.rows(1, 0)[:, :1], 70, D ** -0.5, f"D={D}")
 
 
+@pytest.mark.parametrize("splits", [0, 1, 3])
+@pytest.mark.parametrize("hq,hkv,D,key", [(8, 2, 128, 5), (8, 2, 128, 270), (14, 2, 64, 270), (2, 2, 64, 620), (2, 2, 64, 19)])
+def test_prefill_nan_value_codes(hq, hkv, D, key, splits):
+    """A NaN value code of one KV head makes its column NaN in that head's rows that see it. What else it
+    may reach are the same column and head in earlier rows, at most 256 / (Hq / Hkv) + 62 tokens before."""
+    P, S, col = 20, 700, 9
+    b = Batch(hq, hkv, D, [P, 33], [S, 10], seed=91, spread=0.0)
+    codes = b.codes[1].clone()
+    codes[b.bt[0, key // BS], 1, key % BS, col] = NAN8
+    cache = cw.Fp8KvCache.of(b.cache.k, codes.cuda().view(cw.FP8), b.cache.k_scale, b.cache.v_scale)
+    meta, q = b.meta(), b.queries().cuda()
+
+    def run(c):
+        return _f64(cw.suffix_prefill_attn_fp8(meta, q, c, D ** -0.5) if splits == 0 else
+                    cw.suffix_prefill_attn_split_fp8(meta, q, c, D ** -0.5, num_splits=splits))
+
+    out, clean = run(cache), run(b.cache)
+    sees = np.arange(S) + P >= key
+    far = np.arange(S) + P < key - (256 // (hq // hkv) + 62)
+    nan = np.isnan(out)
+    assert nan[:S][sees, hq // 2:, col].all() and not nan[:S][far].any() and not nan[S:].any()
+    nan[:S, hq // 2:, col] = False
+    assert not nan.any()
+    keep = ~np.isnan(out)
+    assert np.array_equal(out[keep], clean[keep])
+
+
 # ---------------------------------------------------------------- decode attention
 def _check_decode(b, lens, q, out, scale, what):
     for r, n in enumerate(lens):
