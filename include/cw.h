@@ -616,7 +616,8 @@ cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const void* k, int
  * prefix and suffix. Keys and values are code * scale, exactly; q and out are
  * bf16. Probabilities times their value's scale are rounded to bf16 for the
  * product with the codes; softmax and sums are fp32, before the division by the
- * probabilities' sum: values above 2^96 in magnitude may overflow them.
+ * probabilities' sum: values above 2^96 in magnitude may overflow them. A value
+ * scale below 2^-100 (cw_rope_append_fp8 writes none) counts as 2^-100.
  *   plan_host / plan_dev   the unsplit plan of cw_suffix_prefill_plan
  * A table entry outside [0, num_blocks) is read as zero keys and values, each
  * with score 0. A NaN key code makes all outputs of its KV head's query heads NaN

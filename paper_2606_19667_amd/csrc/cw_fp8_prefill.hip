@@ -32,6 +32,9 @@ constexpr int kBlocks = kStep / kBs;
 static_assert(kWaves * 32 == cw::kTileRows, "one 32-column MFMA block per wave");
 static_assert(kWaves == 2 * kBlocks, "a wave stages one block of one tensor");
 constexpr float kMaxSum = 0x1p30f;            // a row's base moves when its sum exceeds this
+// The row's sum is taken from the probabilities times their value's scale. With smaller scales those leave
+// fp32's normal range (at this one probabilities below 2^-26 do) and so does 1 / scale: they count as this one.
+constexpr float kMinValueScale = 0x1p-100f, kMinValueExp = -100.f;
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
@@ -247,7 +250,9 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
       const float scale = raw_keys > 0 ? raw_scale : 1.f;
       float* const s = reinterpret_cast<float*>(lds + at_stage + G::SCALES) + bs;
       if (is_v) {
-        if (lane < 2) s[kBlocks + lane * kBlocks] = lane == 0 ? __builtin_amdgcn_logf(scale) : __builtin_amdgcn_rcpf(scale);
+        if (lane < 2)
+          s[kBlocks + lane * kBlocks] = lane == 0 ? fmaxf(__builtin_amdgcn_logf(scale), kMinValueExp)
+                                                  : fminf(__builtin_amdgcn_rcpf(scale), 1.f / kMinValueScale);
       } else if (lane == 0) {
         *s = a.c_log2 * scale;
       }

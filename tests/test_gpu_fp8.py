@@ -653,6 +653,28 @@ def test_prefill_nan_value_codes(hq, hkv, D, key, splits):
     assert np.array_equal(out[keep], clean[keep])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_of_tiny_scales(D):
+    """Positive scales down to fp32's smallest: such values are nothing beside the others (value scales
+    below 2^-100 count as 2^-100 in the calls over suffix rows: at most 448 * 2^-100 off)."""
+    b = Batch(8, 2, D, [200], [70], seed=92, spread=0.0)
+    tiny = [1e-39, 2.0 ** -149, 2.0 ** -127, 2.0 ** -126, 2.0 ** -101]
+    for j, t in enumerate(tiny):
+        b.scale[0][b.bt[0, 2 * j]] = t
+        b.scale[1][b.bt[0, 2 * j + 1]] = t
+        b.scale[1][b.bt[0, 2 * j], 1] = t
+    cache = cw.Fp8KvCache.of(b.cache.k, b.cache.v, *(s.cuda() for s in b.scale))
+    q = b.queries()
+    meta, qd = b.meta(), q.cuda()
+    for out in (cw.suffix_prefill_attn_fp8(meta, qd, cache, D ** -0.5),
+                cw.suffix_prefill_attn_split_fp8(meta, qd, cache, D ** -0.5, num_splits=3)):
+        _check_attention(_f64(out), _f64(q), b.rows(0, 0), b.rows(1, 0), 200, D ** -0.5, f"tiny scales D={D}")
+    lens = torch.tensor([270], dtype=torch.int32).cuda()
+    for n in (1, 3):
+        out = cw.decode_attn_fp8(qd[-1:], cache, torch.from_numpy(b.bt).cuda(), lens, D ** -0.5, num_splits=n)
+        _check_attention(_f64(out), _f64(q[-1:]), b.rows(0, 0), b.rows(1, 0), 269, D ** -0.5, "decode")
+
+
 # ---------------------------------------------------------------- decode attention
 def _check_decode(b, lens, q, out, scale, what):
     for r, n in enumerate(lens):
