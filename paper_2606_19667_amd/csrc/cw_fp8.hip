@@ -775,6 +775,7 @@ extern "C" cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const v
   if (rope && longest > rope_len)
     return cw::fail(CW_EINVAL, w + ": rope_len " + std::to_string(rope_len) + " is below the longest prompt (" +
                                    std::to_string(longest) + ")");
+  if (longest > INT32_MAX - kBs) return cw::fail(CW_EUNSUPPORTED, w + ": a prompt of 2^31 - 16 tokens or more");
   if (rows == 0) return cw::ok();
   if (units > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
   AppendArgs a;

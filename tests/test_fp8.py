@@ -162,6 +162,15 @@ def test_append_refusals(status, change):
     assert cw.last_error()
 
 
+def test_append_refuses_prompts_that_pass_32_bits():
+    """The kernel counts tokens in 32 bits and drops the rows of such a request; the host says so instead."""
+    big = 2 ** 31 - 20
+    none = dict(q=None, qo=None, rope=None, n=0, stride=2 ** 27 + 4)
+    assert _append(cu=i32(0, 3, 5), pl=i32(7, big), **none) == U and "tokens" in cw.last_error()
+    assert _append(cu=i32(0, 2 ** 30, 2 ** 30 + 1), pl=i32(2 ** 30 - 16, 0), **none) == U
+    assert _append(cu=i32(0, 0, 0), pl=i32(7, big), **none) == cw.CW_OK   # (a request without rows is not touched)
+
+
 def test_append_of_no_rows_launches_nothing():
     assert _append(cu=i32(0, 0, 0), q=None, qo=None, k=None, v=None) == cw.CW_OK
 
