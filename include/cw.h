@@ -602,7 +602,7 @@ cw_status cw_fp8_linear(const void* x8, const float* x_scale, const void* w8, co
  * below the heads' columns or no multiple of 8, q without rope, rope_len below
  * the longest prompt, a misaligned pointer. CW_EUNSUPPORTED: head_dim not
  * 64/128, block_size != 16, more than 65536 KV heads, batch too large, a
- * request with rows that ends at 2^31 - 16 tokens or more. CW_EHIP: launch failure. */
+ * request with rows that ends at 2^31 - 32 tokens or more. CW_EHIP: launch failure. */
 cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                              int64_t v_stride, const float* rope, int32_t rope_len, void* q_out, void* k8, void* v8,
                              float* k_scale, float* v_scale, const int32_t* block_table, int32_t bt_stride,

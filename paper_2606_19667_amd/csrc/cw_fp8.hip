@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp8_kernel(const AppendA
   const int r = s_unit[0];
   if (r < 0) return;
   const int cu0 = a.cu[r], rows = a.cu[r + 1] - cu0, P = a.plen[r];
-  if (P < 0 || P > INT32_MAX - rows - kBs) return;
+  if (P < 0 || P > INT32_MAX - rows - 2 * kBs) return;   // (the end of the block behind the last row is counted too)
   const int lb = P / kBs + s_unit[1];
   const int t_begin = max(P, lb * kBs), t_end = min(P + rows, lb * kBs + kBs);
   if (t_begin >= t_end) return;
@@ -775,7 +775,7 @@ extern "C" cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const v
   if (rope && longest > rope_len)
     return cw::fail(CW_EINVAL, w + ": rope_len " + std::to_string(rope_len) + " is below the longest prompt (" +
                                    std::to_string(longest) + ")");
-  if (longest > INT32_MAX - kBs) return cw::fail(CW_EUNSUPPORTED, w + ": a prompt of 2^31 - 16 tokens or more");
+  if (longest > INT32_MAX - 2 * kBs) return cw::fail(CW_EUNSUPPORTED, w + ": a prompt of 2^31 - 32 tokens or more");
   if (rows == 0) return cw::ok();
   if (units > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
   AppendArgs a;

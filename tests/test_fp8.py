@@ -164,7 +164,7 @@ def test_append_refusals(status, change):
 
 def test_append_refuses_prompts_that_pass_32_bits():
     """The kernel counts tokens in 32 bits and drops the rows of such a request; the host says so instead."""
-    big = 2 ** 31 - 20
+    big = 2 ** 31 - 34   # two rows behind it end at 2^31 - 32
     none = dict(q=None, qo=None, rope=None, n=0, stride=2 ** 27 + 4)
     assert _append(cu=i32(0, 3, 5), pl=i32(7, big), **none) == U and "tokens" in cw.last_error()
     assert _append(cu=i32(0, 2 ** 30, 2 ** 30 + 1), pl=i32(2 ** 30 - 16, 0), **none) == U
