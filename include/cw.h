@@ -619,6 +619,8 @@ cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const void* k, int
  * probabilities' sum: values above 2^96 in magnitude may overflow them. A value
  * scale below 2^-100 (cw_rope_append_fp8 writes none) counts as 2^-100.
  *   plan_host / plan_dev   the unsplit plan of cw_suffix_prefill_plan
+ * The call never cuts a tile's keys: for few rows behind long prefixes the caller
+ * takes cw_suffix_prefill_attn_split_fp8.
  * A table entry outside [0, num_blocks) is read as zero keys and values, each
  * with score 0. A NaN key code makes all outputs of its KV head's query heads NaN
  * in the rows that see it, and no others; a NaN value code its column of them. A NaN

@@ -67,8 +67,8 @@ __device__ __forceinline__ float wave_sum(float x) {
 // TPR threads work on a row (64: a wave, four rows a workgroup; 256: the workgroup), each on
 // CH pieces of 8 columns TPR apart, so that 16 neighbouring lanes hold a group of 128 columns
 // and its maximum takes four exchanges. Sums are fp32.
-// HBM-bound: 7 bytes a column with a residual. 16,128 rows of 4,096: 80.5 us, 5.8 TB/s (a copy of 1 GiB
-// 5.2); 64 rows 3.8 us in a captured graph, one chain of load, sum, maximum and store.
+// HBM-bound: 7 bytes a column with a residual. 16,128 rows of 4,096: 80.5 us, 5.8 TB/s, from the same rows each
+// time or from four sets in turn (1.9 GB; a copy, which writes as much as it reads, makes 4.7 to 5.3); 64 rows 3.8 us in a captured graph, one chain of load, sum, maximum and store.
 // ---------------------------------------------------------------------------
 struct NormArgs {
   const uint16_t* x;
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kThreads) void add_rms_norm_fp8_kernel(const NormAr
 // lies in one lane, and a block's maximum is a wave reduction. Heads are queries, keys, then
 // values; a wave keeps the cosines and sines of its rows over all its heads.
 // HBM-bound: reads 2 (Hq + 2 Hkv) D bytes a row, writes 2 Hq D + 2 Hkv D. 16,128 rows of 48 heads of 128:
-// 88 us, 4.4 TB/s with the rotation table (a copy of 1 GiB 5.2; what is missing are the ends of the
+// 88 us, 4.4 TB/s with the rotation table (a copy 4.7 to 5.3; what is missing are the ends of the
 // workgroups, each a chain of offsets, table word, rows, maximum, store); 64 requests of one row: 6.9 us in a
 // captured graph, 13.9 called one by one, which is the host's time.
 // ---------------------------------------------------------------------------
@@ -408,9 +408,12 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp8_kernel(const AppendA
 //  * V^T comes from bf16 rows in LDS by transposing reads (ds_read_b64_tr_b16). The rows of
 //    a wave are its own: no barrier in the loop.
 //  * K's scale multiplies the scores and V's the probabilities before they are rounded to
-//    bf16 for the product; sums are fp32.
+//    bf16 for the product, which reads bf16; sums are fp32. The row's sum takes the probabilities
+//    unrounded (they are at hand, and V's scale is not in them): the outputs' relative rms error
+//    against 64 bits is 0.0017 to 0.0018, of which the outputs' own rounding is 0.0017.
 // HBM-bound when sequences are long: 64 requests of about 10,367 tokens, 8 KV heads of 128 (1.37 GB) 283 us,
-// 4.85 TB/s (a copy of 1 GiB 5.2). 16 of about 1,407 (46 MB) 16.0 us, 2.9 TB/s: there the chain of length,
+// 4.85 TB/s (a copy 4.7 to 5.3). 16 of about 1,407 (46 MB) 16.0 us, 2.9 TB/s, from the last-level cache (from
+// 16 caches in turn, which it does not hold, 17.3): there the chain of length,
 // table word, codes, softmax and the join of the runs bounds it, with two launches. The launch bounds name two
 // waves a SIMD: left to itself the compiler takes fewer registers and the kernel is 25 % slower.
 // ---------------------------------------------------------------------------
