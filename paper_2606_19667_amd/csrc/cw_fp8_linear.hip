@@ -569,10 +569,10 @@ void fp8_linear_tile_kernel(const LinearArgs a) {
 // on several cards).
 //
 // What bounds them: up to 64 tokens the read of W (25 MB in 6.5 us, 3 of them start and end of a
-// workgroup, where the last-level cache holds W; 9.2 from HBM); the tiles of 64 to 128 the copies into LDS (96 KB in flight a CU, about 60 GB/s each, 11
-// TB/s over all), so that a step of 128 x 128 takes 1,200 cycles beside 512 of products; 256 x 256 the
-// vector work beside the products: an interval takes 816 cycles, 665 without the scaling, 512 of them
-// matrix work (matrix pipe busy 57 %, clock 1.94 GHz).
+// workgroup, where the last-level cache holds W; 9.2 from HBM); the tiles of 64 to 128 the copies into LDS
+// (96 KB in flight a CU, about 60 GB/s each, 11 TB/s over all), so that a step of 128 x 128 takes 1,200
+// cycles beside 512 of products; 256 x 256 the vector work beside the products: an interval takes 816
+// cycles, 665 without the scaling, 512 of them matrix work (matrix pipe busy 57 %, clock 1.94 GHz).
 struct LinearShape {
   int tile_f, tile_t;
   bool persistent;
