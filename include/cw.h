@@ -580,9 +580,9 @@ cw_status cw_fp8_linear(const void* x8, const float* x_scale, const void* w8, co
  *   head, with amax their largest finite magnitude,
  *     need  = 2^e, e the smallest in [-100, 120] with amax <= 448 * 2^e
  *     scale = need where the call writes the block's slot 0, else
- *             max(the block's scale, need): then the block's earlier rows are
- *             rounded to the new scale (exact but for values below the
- *             smallest normal code)
+ *             max(the block's scale, need): where that is need, the block's
+ *             earlier rows are rounded to it (where the block's scale is a power
+ *             of two, exact but for values below the smallest normal code)
  *     code  = e4m3(value / scale); infinite and NaN values are NaN codes
  * Slots behind a request's last token and all other blocks keep their bytes. A
  * table entry outside [0, num_blocks) drops its tokens. No two requests may

@@ -195,8 +195,8 @@ __global__ __launch_bounds__(kThreads) void add_rms_norm_fp8_kernel(const NormAr
 // lies in one lane, and a block's maximum is a wave reduction. Heads are queries, keys, then
 // values; a wave keeps the cosines and sines of its rows over all its heads.
 // HBM-bound: reads 2 (Hq + 2 Hkv) D bytes a row, writes 2 Hq D + 2 Hkv D. 16,128 rows of 48 heads of 128:
-// 88 us, 4.4 TB/s with the rotation table (a copy 4.7 to 5.3; what is missing are the ends of the
-// workgroups, each a chain of offsets, table word, rows, maximum, store); 64 requests of one row: 6.9 us in a
+// 84 us, 4.6 TB/s with the rotation table (a copy 4.7 to 5.3; what is missing are the ends of the
+// workgroups, each a chain of offsets, table word, rows, maximum, store); 64 requests of one row: 6.7 us in a
 // captured graph, 13.9 called one by one, which is the host's time.
 // ---------------------------------------------------------------------------
 struct AppendArgs {
@@ -232,9 +232,25 @@ __device__ __forceinline__ void rotate(float& x, float& y, f32x2 turn) {
   y = w * turn[0] + u * turn[1];
 }
 
+// A result v that lies `rest` (or a positive multiple of it) off the exact one, with its last bit set to one where
+// they differ: rounded on to fewer bits it goes where the exact result goes, as it is never halfway by rounding alone.
+__device__ __forceinline__ float to_odd(float v, float rest) {
+  const uint32_t b = __float_as_uint(v);
+  if (rest == 0.f || (b & 1) != 0 || !(fabsf(v) > 0x1p-60f)) return v;   // (a code of so small a value is zero)
+  return __uint_as_float((rest > 0.f) == (v > 0.f) ? b + 1 : b - 1);
+}
+// x / s by its inverse (inv = 1 / s rounded).
+__device__ __forceinline__ float quotient(float x, float s, float inv) {
+  const float q = x * inv, r = fmaf(-q, s, x);
+  if (r == 0.f) return q;
+  const float p = fmaf(r, inv, q);
+  return to_odd(p, fmaf(-p, s, x));
+}
+
 __device__ __forceinline__ uint32_t rescale_fp8x4(uint32_t w, float f) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), true);
-  return pack_fp8x4(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+  auto times = [f](float c) __attribute__((always_inline)) { return to_odd(c * f, fmaf(c, f, -(c * f))); };
+  return pack_fp8x4(times(lo[0]), times(lo[1]), times(hi[0]), times(hi[1]));
 }
 
 template <int D>
@@ -362,8 +378,8 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp8_kernel(const AppendA
       if (had >= scale) {
         scale = had;
       } else if (t < t_begin) {
-        // The same values at the larger scale: exact but for values that fall below the
-        // smallest normal code, as both scales are powers of two.
+        // The same values at the larger scale: where both scales are powers of two (this call's are),
+        // exact but for values that fall below the smallest normal code.
         const float f = had / scale;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -374,12 +390,12 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp8_kernel(const AppendA
       }
     }
     const float inv = 1.f / scale;
-    if (live) {
+    auto put = [&](auto code) __attribute__((always_inline)) {
       uint32_t o0[W / 4], o1[W / 4];
 #pragma unroll
       for (int i = 0; i < W / 4; ++i) {
-        o0[i] = pack_fp8x4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
-        o1[i] = pack_fp8x4(y[4 * i] * inv, y[4 * i + 1] * inv, y[4 * i + 2] * inv, y[4 * i + 3] * inv);
+        o0[i] = pack_fp8x4(code(x[4 * i]), code(x[4 * i + 1]), code(x[4 * i + 2]), code(x[4 * i + 3]));
+        o1[i] = pack_fp8x4(code(y[4 * i]), code(y[4 * i + 1]), code(y[4 * i + 2]), code(y[4 * i + 3]));
       }
       if constexpr (W == 16) {
         *reinterpret_cast<u32x4*>(dst) = u32x4{o0[0], o0[1], o0[2], o0[3]};
@@ -388,6 +404,12 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp8_kernel(const AppendA
         *reinterpret_cast<u32x2*>(dst) = u32x2{o0[0], o0[1]};
         *reinterpret_cast<u32x2*>(dst + D / 2) = u32x2{o1[0], o1[1]};
       }
+    };
+    if (live) {
+      if (__builtin_expect((__float_as_uint(scale) & 0x7FFFFFu) == 0, 1))
+        put([&](float v) __attribute__((always_inline)) { return v * inv; });
+      else   // (a scale of the caller's, no power of two)
+        put([&](float v) __attribute__((always_inline)) { return quotient(v, scale, inv); });
     }
     if (lane == 0) *scale_at = scale;
   }
@@ -805,8 +827,8 @@ extern "C" cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const v
   a.rope_len = rope_len;
   // Heads over grid y: a workgroup per CU at least, and two per unit, so that the last round of a
   // large batch is short; more share the rows' cosines and sines less. us for 1, 2, 3, 4, 6, 12 per unit:
-  // 1,030 units of 48 heads 93.6, 87.6, 88.4, 96.2, 88.7, 108.1; 64 units 14.9, 9.4, 8.4, 6.9, 7.4, 7.8;
-  // 160 units of 36 heads 14.1, 12.5, 11.7, 12.9, 12.5, 14.2.
+  // 1,030 units of 48 heads 94.3, 84.0, 84.6, 96.4, 85.2, 102.3; 64 units 14.8, 9.4, 8.2, 6.7, 7.0, 7.5;
+  // 160 units of 36 heads 13.8, 12.0, 11.0, 12.3, 13.0, 13.6.
   const int64_t heads = a.hq + 2 * int64_t(num_kv_heads), full = (heads + kWaves - 1) / kWaves;
   const int64_t gy = std::min({full, int64_t(65535), std::max<int64_t>(2, (cw::kNumCu + units - 1) / units)});
   auto* const s = static_cast<hipStream_t>(stream);

@@ -412,6 +412,40 @@ def test_append_drops_blocks_outside_the_pool():
     _check_append(b, None, k, v, None, None, "foreign blocks")
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_into_blocks_whose_scale_is_no_power_of_two(D):
+    """Rows that follow others in a block of any scale: quotients (and, where the scale is raised, products of the
+    earlier codes) a rounding away from halfway between two codes go to the nearest code, not to the even one."""
+    halves = [t for t in (F.decode(np.arange(0x20, 0x70, 5)) + F.decode(np.arange(0x21, 0x71, 5))) / 2]
+    near = [np.float32(1 / t) for t in halves] + [np.float32(t / 1.125) for t in halves]
+    scales = [f(x) for x in near for f in (lambda x: np.nextafter(x, np.float32(0)), np.float32,
+                                           lambda x: np.nextafter(x, np.float32(9e9)))]
+    n = len(scales)
+    g = _gen(93)
+    signs = (torch.randint(0, 2, (n, 1, D), generator=g) * 2 - 1).float()
+    rows = torch.exp2(torch.randint(-4, 5, (n, 1, D), generator=g).float()) * signs
+    for grow in (False, True):
+        codes = [torch.randint(0, 256, (n, 1, BS, D), generator=g, dtype=torch.uint8) for _ in range(2)]
+        for c in codes:   # earlier codes 1.125 and others; behind the new row NaN
+            c[:, :, :7, ::2] = 0x39
+            c[:, :, 8:] = NAN8
+        scale = [torch.tensor(np.array(scales)).view(n, 1).clone() for _ in range(2)]
+        cache = cw.Fp8KvCache.of(*(c.cuda().view(cw.FP8) for c in codes), *(x.cuda() for x in scale))
+        new = rows.clone()
+        if grow:   # the scale becomes the smallest power of two above it, times 4
+            up = torch.exp2(torch.floor(torch.log2(scale[0].double())) + 3).float()
+            new[:, :, :1] = (up * 448).view(n, 1, 1).flip(0)   # (request r writes block n - 1 - r)
+        new = new.to(torch.bfloat16)
+        bt = np.arange(n, dtype=np.int32)[::-1].copy()[:, None]
+        meta = cw.BatchMeta(bt, np.arange(n + 1), [7] * n, 1, 1, D)
+        cw.rope_append_fp8(meta, new.cuda(), (-new).cuda(), cache)
+        for c, s, x, got, gs in ((codes[0], scale[0], new, cache.k, cache.k_scale),
+                                 (codes[1], scale[1], -new, cache.v, cache.v_scale)):
+            values, es = F.append(F.decode(c.numpy()), s.double().numpy(), x, bt, np.arange(n + 1), [7] * n)
+            assert np.array_equal(_f64(gs), es) and (es > s.double().numpy()).all() == grow
+            assert np.array_equal(F.decode(_codes(got)), values, equal_nan=True), grow
+
+
 def test_append_captured_and_replayed_with_growing_prefixes():
     """A decode step's append in a HIP graph: each replay reads the prefix lengths and the
     table from device memory and equals an eager call at those lengths."""
@@ -911,6 +945,37 @@ def test_layer_on_given_streams():
             seg = [m for m in torch.cuda.memory_snapshot()
                    if m["address"] <= a.data_ptr() < m["address"] + m["total_size"]]
             assert [m["stream"] for m in seg] == [s.cuda_stream], i
+
+
+def test_blocks_beyond_32_bit_offsets():
+    """Blocks at the end of a cache of 5.7 GB a tensor: append, prefill (whole and in runs) and decode have the
+    bits that they have in a small one."""
+    nb, hkv, D, hq, S = 600000, 5, 128, 15, [300, 70]
+    g = _gen(94)
+    big = np.full((2, 25), -1, np.int32)
+    small = big.copy()
+    order = torch.randperm(26, generator=g).numpy()
+    ids = np.concatenate([np.arange(nb - 20, nb), [0, 1, 2 ** 18 - 1, 2 ** 18, 2 ** 18 + 1, nb // 2]])[order]
+    for r, (a, n) in enumerate(((0, 19), (19, 5))):
+        big[r, :n], small[r, :n] = ids[a:a + n], np.arange(a, a + n)
+    rope = torch.from_numpy(cw.rope_table(512, D, 10000.0)).cuda()
+    qkv = _normal(g, sum(S), (hq + 2 * hkv) * D).cuda()
+    q, k, v = (t.view(sum(S), -1, D) for t in qkv.split([hq * D, hkv * D, hkv * D], 1))
+    lens = torch.tensor(S, dtype=torch.int32).cuda()
+    res = []
+    for n, table in ((nb, big), (26, small)):
+        cache = cw.Fp8KvCache(n, hkv, D)
+        meta = cw.BatchMeta(table, np.concatenate([[0], np.cumsum(S)]), [0, 0], hq, hkv, D)
+        qr = cw.rope_append_fp8(meta, k, v, cache, q=q, rope=rope)
+        out = [qr, cw.suffix_prefill_attn_fp8(meta, qr, cache, 0.088),
+               cw.suffix_prefill_attn_split_fp8(meta, qr, cache, 0.088, num_splits=3)]
+        out += [cw.decode_attn_fp8(qr[:2], cache, meta.bt, lens, 0.088, num_splits=m) for m in (1, 4)]
+        full = torch.from_numpy(np.concatenate([table[0, :18], table[1, :4]])).cuda().long()   # whole blocks
+        out += [c.view(torch.uint8)[full] for c in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+        res.append(out)
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(*res)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
 
 
 def test_decode_calls_at_once_on_two_streams():
