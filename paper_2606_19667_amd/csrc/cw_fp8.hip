@@ -435,7 +435,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp8_kernel(const AppendA
 //    against 64 bits is 0.0017 to 0.0018, of which the outputs' own rounding is 0.0017.
 // HBM-bound when sequences are long: 64 requests of about 10,367 tokens, 8 KV heads of 128 (1.37 GB) 283 us,
 // 4.85 TB/s (a copy 4.7 to 5.3). 16 of about 1,407 (46 MB) 16.0 us, 2.9 TB/s, from the last-level cache (from
-// 16 caches in turn, which it does not hold, 17.3): there the chain of length,
+// 12 caches in turn, which it does not hold, 18.1): there the chain of length,
 // table word, codes, softmax and the join of the runs bounds it, with two launches. The launch bounds name two
 // waves a SIMD: left to itself the compiler takes fewer registers and the kernel is 25 % slower.
 // ---------------------------------------------------------------------------

@@ -565,11 +565,11 @@ void fp8_linear_tile_kernel(const LinearArgs a) {
 // within 8.3 % of the best shape at each and 0.24 % on average; leaving out one shape costs 9 % (32 x 16)
 // to 87 % (128 x 128) at its sizes. Examples, us, 6,144 features, depth 4,096, the 128 x 128 tile
 // against the chosen one: T = 16: 17.2 / 6.5 (32 x 16); 64: 17.6 / 9.5 (32 x 64); 128: 18.3 / 11.4
-// (64 x 64); 256: 18.9; 1,024: 40; 4,096: 127 / 104 (256 x 256); 16,128: 494 / 345 (2.36 PFLOP/s; 345 to 375
+// (64 x 64); 256: 18.9; 1,024: 40; 4,096: 127 / 104 (256 x 256); 16,128: 494 / 345 (2.36 PFLOP/s; 334 to 375
 // on several cards).
 //
 // What bounds them: up to 64 tokens the read of W (25 MB in 6.5 us, 3 of them start and end of a
-// workgroup, where the last-level cache holds W; 9.2 from HBM); the tiles of 64 to 128 the copies into LDS
+// workgroup, where the last-level cache holds W; 9.7 from HBM); the tiles of 64 to 128 the copies into LDS
 // (96 KB in flight a CU, about 60 GB/s each, 11 TB/s over all), so that a step of 128 x 128 takes 1,200
 // cycles beside 512 of products; 256 x 256 the vector work beside the products: an interval takes 816
 // cycles, 665 without the scaling, 512 of them matrix work (matrix pipe busy 57 %, clock 1.94 GHz).
