@@ -44,9 +44,10 @@ __device__ __forceinline__ u32x2 widen_fp8x4(uint32_t w) {
   return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false)),
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true))};
 }
+// (Maxima that a NaN passes through: with NaN honoured fmaxf would quiet each operand first.)
 __device__ __forceinline__ float max_pair32(float x) {   // of this lane and lane ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float sum_pair32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -349,8 +350,8 @@ void suffix_prefill_fp8_kernel(const PrefillArgs a) {
     for (int b = 0; b < kBlocks; ++b) {
       float y = sc[b >> 1][(b & 1) * 8];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) y = fmaxf(y, sc[b >> 1][(b & 1) * 8 + i]);
-      mx = fmaxf(mx, y * kc[b]);
+      for (int i = 1; i < 8; ++i) y = __builtin_elementwise_maximum(y, sc[b >> 1][(b & 1) * 8 + i]);
+      mx = __builtin_elementwise_maximum(mx, y * kc[b]);
     }
     return max_pair32(mx);
   };
