@@ -686,6 +686,177 @@ cw_status cw_decode_attn_fp8(const void* q, const void* k8, const void* v8, cons
                              int32_t head_dim, int32_t block_size, int32_t num_blocks, float softmax_scale,
                              int32_t num_splits, void* workspace, int64_t workspace_bytes, void* out, void* stream);
 
+/* ========================================================================
+ * The 4-bit cache. With a reused prefix only the suffix is prefilled (paper
+ * Sec. 1 and 2.1), and what can be reused is what the cache holds (Sec. 3.4:
+ * the engine evicts when its memory is full): in 4 bits it holds 3.76 times the
+ * prefix blocks of a bf16 cache, 1.88 times those of the 8-bit one. The calls
+ * below append to it (with the position rotation on the way), read rows back and
+ * attend over it, for prompts and for single tokens.
+ *
+ * 4-bit values are e2m1 (OCP: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; the
+ * codes 0 .. 7, plus 8 for the sign). Each token, KV head and 32 columns have one
+ * scale 2^(c - 127), held as the byte c; c = 255 makes all 32 values NaN. A value
+ * is code times scale.
+ *
+ *   pages   bytes [num_blocks, Hkv, 17 D]: a page is one (block of 16 tokens,
+ *           KV head) in one piece, with (T: token of the block, d: column)
+ *     keys      code of (T, d) in byte T D/2 + d/2
+ *     values    byte 8 D + ((T/4 16 + d/(D/16)) 4 + T%4) D/32 + d%(D/16)/2
+ *               (both: the lower 4 bits hold the even column)
+ *     scales    keys: byte 16 D + T D/32 + d/32
+ *               values: byte 16 D + D/2 + d/32 16 + T
+ * Values are laid out as the matrix instructions read them. A page holds nothing
+ * but these bytes: blocks can be copied, shared and moved between pools as they
+ * are. Prefix lengths need not be multiples of 16 in these calls. Pointers are
+ * 16-byte aligned except those of int32 arrays. Device calls are asynchronous on
+ * `stream`, and on the device that it belongs to, which has to be the current one.
+ * ======================================================================== */
+
+/* ------------------------------------------------------------------------
+ * Device: rotary embedding of the suffix rows' queries and keys and the append
+ * of keys and values to the 4-bit cache (paper Sec. 2.1: KV memory managed in
+ * fixed-size blocks). Suffix row i of request r is token p = P_r + i. With n =
+ * rotary_dim / 2 pairs of columns (a, b), (j, j + n) or, interleaved,
+ * (2 j, 2 j + 1), j < n:
+ *   rot(u)[a] = u[a] cos_pj - u[b] sin_pj,  rot(u)[b] = u[b] cos_pj + u[a] sin_pj
+ * and the columns from rotary_dim on stay as they are.
+ *   q_out[t][h] = bf16(rot(q[t][h])), rotated in fp32
+ *   K rows rot(k[t][g]), V rows v[t][g], 32 columns at a time, with amax their
+ *     largest magnitude:
+ *     scale = 2^e, e the smallest in [-100, 125] with amax <= 7 * 2^e
+ *     code  = the e2m1 value nearest to value / scale, halfway to the even code,
+ *             6 beyond it
+ *   The values are those of exact arithmetic on the bf16 rows and the fp32 table:
+ *   one next to a border of two codes falls on its side of it. 32 columns with an
+ *   infinite or NaN value (or one that leaves fp32) have scale byte 255, codes 0.
+ * No token's codes depend on another's. Other tokens' bytes of a block, slots
+ * behind a request's last token and all other blocks keep their bytes. A table
+ * entry outside [0, num_blocks) drops its tokens. Two requests may write the same
+ * block if their tokens lie in different slots of it.
+ *   q, k, v     device bf16 rows of Hq / Hkv heads of D values, q_stride /
+ *               k_stride / v_stride elements apart (slices of one projection)
+ *   q_out       device bf16 [total_s, Hq, D]; q and q_out both NULL: no queries.
+ *               q_out may be q itself where q_stride is Hq D.
+ *   rope        device fp32 [rope_len, rotary_dim / 2, 2]: (cos, sin), as
+ *               cw_rope_table(rope_len, rotary_dim, base) writes it or with other
+ *               angles (scaled for long contexts) or sizes; NULL: keys are stored
+ *               as they are (and q must be NULL)
+ *   rotary_dim  a multiple of 16 in [16, D]; unused without rope
+ *   interleaved 0 or 1
+ *   cu_suffix, prefix_len   as for cw_kv_append. The launch depends on
+ *               cu_suffix alone: a captured call can be replayed with other
+ *               prefix lengths in prefix_len_dev (at most rope_len and
+ *               16 * bt_stride tokens with the suffix; beyond, tokens are
+ *               dropped or rotated by the last position, never a fault).
+ * CW_EINVAL: NULL pointer, batch < 1, num_kv_heads < 1, P_r < 0, cu not
+ * non-decreasing from 0, ceil(L_r / 16) > bt_stride, num_blocks < 1, a stride
+ * below the heads' columns or no multiple of 8, q without rope, rotary_dim or
+ * interleaved out of range, q_out at q's address with rows that lie apart,
+ * rope_len below the longest prompt, a misaligned pointer. CW_EUNSUPPORTED:
+ * head_dim not 64/128, block_size != 16, more than 65536 KV heads, batch too
+ * large, a request with rows that ends at 2^31 - 32 tokens or more. CW_EHIP:
+ * launch failure. */
+cw_status cw_rope_append_fp4(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, const float* rope, int32_t rope_len, int32_t rotary_dim,
+                             int32_t interleaved, void* q_out, void* pages, const int32_t* block_table,
+                             int32_t bt_stride, const int32_t* cu_suffix_dev, const int32_t* prefix_len_dev,
+                             const int32_t* cu_suffix_host, const int32_t* prefix_len_host, int32_t batch,
+                             int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                             int32_t num_blocks, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: rows of the 4-bit cache as bf16 (a prefix that is to go into another
+ * cache, or to be looked at). Row cu[r] + i is token first[r] + i of request r,
+ * i < cu[r + 1] - cu[r]:
+ *   k_rows, v_rows[cu[r] + i][g][:] = the values of keys and values, exactly (a
+ *   value beyond bf16's largest is infinite; scales below 2^-100, which
+ *   cw_rope_append_fp4 does not write, may be read as zeros)
+ * A table entry outside [0, num_blocks) is read as zeros. The launch depends on
+ * cu alone, as the append's does.
+ *   cu_rows     int32 [batch + 1], first int32 [batch], on the host and on the
+ *               device, with the checks of cu_suffix and prefix_len
+ *   k_rows, v_rows   device bf16 [cu[batch], Hkv, D]; either may be NULL: not wanted
+ * Errors as cw_rope_append_fp4's of these arguments. */
+cw_status cw_cache_rows_fp4(const void* pages, const int32_t* block_table, int32_t bt_stride,
+                            const int32_t* cu_rows_dev, const int32_t* first_dev, const int32_t* cu_rows_host,
+                            const int32_t* first_host, int32_t batch, int32_t num_kv_heads, int32_t head_dim,
+                            int32_t block_size, int32_t num_blocks, void* k_rows, void* v_rows, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: cw_suffix_prefill_attn over the 4-bit cache, which must already hold
+ * prefix and suffix. Keys and values are code * scale, exactly; q and out are
+ * bf16. Probabilities are rounded to bf16 for the product; softmax and sums are
+ * fp32, before the division by the probabilities' sum: values above 2^96 in
+ * magnitude may overflow them. Scales below 2^-100 (cw_rope_append_fp4 writes
+ * none) may be read as zeros.
+ *   plan_host / plan_dev   the unsplit plan of cw_suffix_prefill_plan
+ * The call never cuts a tile's keys: for few rows behind long prefixes the caller
+ * takes cw_suffix_prefill_attn_split_fp4.
+ * A table entry outside [0, num_blocks) is read as zero keys and values, each
+ * with score 0. A NaN scale of keys makes all outputs of its KV head's query heads
+ * NaN in the rows that see the token, and no others; one of values its 32 columns
+ * of them. A NaN scale of a suffix row's values can also reach (0 times NaN in the
+ * matrix product) the same columns in earlier rows of the request, those at most
+ * 256 / (Hq / Hkv) + 62 tokens before it. Codes and scales behind a prompt's end
+ * are never used.
+ * Errors as cw_suffix_prefill_attn (P_r need not be a multiple of 16), plus
+ * CW_EINVAL for a misaligned pointer. */
+cw_status cw_suffix_prefill_attn_fp4(const void* q, const void* pages, const int32_t* block_table, int32_t bt_stride,
+                                     const int32_t* cu_suffix_host, const int32_t* prefix_len_host, int32_t batch,
+                                     int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                     int32_t block_size, int32_t num_blocks, float softmax_scale,
+                                     const int32_t* plan_host, const int32_t* plan_dev, void* out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: cw_suffix_prefill_attn_fp4 with each tile's keys in runs, for few
+ * suffix rows behind long prefixes (a question after cached evidence), as
+ * cw_suffix_prefill_attn_split is of cw_suffix_prefill_attn: a plan of
+ * cw_suffix_prefill_plan with num_splits runs; the runs' parts are combined as
+ * by cw_lse_merge.
+ *   workspace   device, 16-byte aligned, at least
+ *               cw_suffix_prefill_split_workspace_bytes(total_s, Hq, D, num_splits)
+ *               bytes; overwritten. Calls that may run at the same time need
+ *               workspaces of their own.
+ * Errors as cw_suffix_prefill_attn_fp4, plus CW_EINVAL for a missing, too small
+ * or misaligned workspace. */
+cw_status cw_suffix_prefill_attn_split_fp4(const void* q, const void* pages, const int32_t* block_table,
+                                           int32_t bt_stride, const int32_t* cu_suffix_host,
+                                           const int32_t* prefix_len_host, int32_t batch, int32_t num_q_heads,
+                                           int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                                           int32_t num_blocks, float softmax_scale, const int32_t* plan_host,
+                                           const int32_t* plan_dev, void* workspace, int64_t workspace_bytes,
+                                           void* out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Device: attention of one query row per request over the 4-bit cache (the next
+ * token after a prefill). For request r, query head h (KV head g = h / (Hq / Hkv)):
+ *   s_j = softmax_scale * <q[r, h, :], K_r[j, g, :]>, j = 0 .. seq_lens[r] - 1
+ *   out[r, h, :] = sum_j softmax(s)_j V_r[j, g, :]     (zeros for length 0)
+ * Lengths are read from device memory alone, and the launch does not depend on
+ * them: a captured call can be replayed as sequences grow. A length above
+ * 16 * bt_stride counts as that, one below 0 as 0. Table entries outside the
+ * pool, NaN scales and values above 2^96 as for cw_suffix_prefill_attn_fp4.
+ *   q, out       device bf16 [batch, Hq, D]
+ *   seq_lens_dev device int32 [batch]
+ *   num_splits   1 .. 64 runs that each sequence is cut into, combined as by
+ *                cw_lse_merge (for few requests with long sequences)
+ *   workspace    device, 16-byte aligned, at least
+ *                cw_decode_attn_fp4_workspace_bytes(batch, Hq, D, num_splits)
+ *                bytes (0 for one split: NULL); overwritten. Calls that may run
+ *                at the same time need workspaces of their own.
+ * CW_EINVAL: NULL pointer, batch < 1, Hq % Hkv != 0, num_blocks or bt_stride < 1,
+ * softmax_scale not finite and positive, num_splits out of range, a missing or
+ * too small workspace, a misaligned pointer. CW_EUNSUPPORTED: head_dim not
+ * 64/128, block_size != 16, Hq / Hkv > 128, more than 65536 KV heads, sequences
+ * of 2^31 - 4096 tokens or more, batch too large. CW_EHIP: launch failure. */
+int64_t cw_decode_attn_fp4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t head_dim,
+                                           int32_t num_splits);
+cw_status cw_decode_attn_fp4(const void* q, const void* pages, const int32_t* block_table, int32_t bt_stride,
+                             const int32_t* seq_lens_dev, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                             int32_t head_dim, int32_t block_size, int32_t num_blocks, float softmax_scale,
+                             int32_t num_splits, void* workspace, int64_t workspace_bytes, void* out, void* stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement aid (not a step of the path). A roofline of the attention kernel
  * prices it against the data-sheet bf16 peak; the rate this card sustains

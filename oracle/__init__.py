@@ -16,6 +16,8 @@ Modules
              Eq. 1) and the baseline orders (Sec. 4).
   fp8        e4m3 values, the norm with 8-bit rows, the block-scaled product and the
              append into an 8-bit cache.
+  fp4        e2m1 values with a scale per 32 columns, the 4-bit cache's pages, the rotation
+             of part of a head and the append.
   projection the suffix QKV projection with rotary position embedding (the
              per-layer work that feeds the cache append and attention).
 
@@ -24,6 +26,7 @@ The only blocking anywhere is the independent-row chunking in `attention`, which
 bounds memory and does not change any row's arithmetic.
 
 Parity status: every function here is pinned by tests/test_oracle_pins.py,
-tests/test_ordering.py, tests/test_projection.py and tests/test_fp8.py (brute force, closed forms, a library routine, published test vectors, the
+tests/test_ordering.py, tests/test_projection.py, tests/test_fp8.py and
+tests/test_fp4.py (brute force, closed forms, a library routine, published test vectors, the
 paper's worked examples). No function is "parity unpinned".
 """

@@ -30,7 +30,7 @@ ARCH = "gfx950"
 
 HOST_SOURCES = ["cw_host.cpp", "cw_tree.cpp", "cw_proj.cpp"]
 HIP_SOURCES = ["cw_kernels.hip", "cw_qkv.hip", "cw_probe.hip", "cw_fp8.hip", "cw_fp8_prefill.hip",
-               "cw_fp8_linear.hip"]
+               "cw_fp8_linear.hip", "cw_fp4.hip", "cw_fp4_prefill.hip"]
 
 HIP_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
@@ -48,14 +48,16 @@ HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra"]
 # branches only; structurizing them makes the register allocator keep two
 # copies of the 64-register output accumulator across the branch arms, which
 # overflows the 256-register budget of two waves per SIMD. The calls of the
-# 8-bit path promise where NaN codes and values go, so comparisons with NaN have
+# 8-bit path and over the 4-bit cache promise where NaN codes, scales and values go, so comparisons with NaN have
 # to mean what they say there (the product's code is the same either way, the
 # prefill takes the same time). Runs of keys are joined by cw_kernels.hip, which
 # only multiplies and adds their values: a NaN log-sum-exp does not get there.
 EXTRA_FLAGS = {"cw_kernels.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"],
                "cw_fp8_prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true", "-fhonor-nans"],
                "cw_fp8_linear.hip": ["-fhonor-nans"],
-               "cw_fp8.hip": ["-fhonor-nans"]}
+               "cw_fp8.hip": ["-fhonor-nans"],
+               "cw_fp4_prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true", "-fhonor-nans"],
+               "cw_fp4.hip": ["-fhonor-nans"]}
 
 
 def _run(cmd):

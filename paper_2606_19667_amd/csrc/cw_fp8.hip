@@ -839,6 +839,14 @@ extern "C" cw_status cw_rope_append_fp8(const void* q, int64_t q_stride, const v
   return check_launch("rope_append_fp8 launch");
 }
 
+cw_status cw::decode_join(const char* what, int32_t head_dim, const float* part_o, const float* part_lse,
+                          int32_t parts, int64_t rows, void* out, void* stream) {
+  auto* const kernel = head_dim == 128 ? decode_join_kernel<128> : decode_join_kernel<64>;
+  hipLaunchKernelGGL(kernel, dim3(unsigned(rows)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), part_o,
+                     part_lse, parts, rows, static_cast<uint16_t*>(out));
+  return check_launch((std::string(what) + " join launch").c_str());
+}
+
 namespace {
 int64_t decode_lse_offset(int64_t rows, int head_dim, int num_splits) {
   return (int64_t(num_splits) * rows * head_dim * 4 + 255) / 256 * 256;
@@ -911,11 +919,5 @@ extern "C" cw_status cw_decode_attn_fp8(const void* q, const void* k8, const voi
     hipLaunchKernelGGL(decode_attn_fp8_kernel<64>, dim3(unsigned(grid)), dim3(kThreads), 0, s, a);
   st = check_launch("decode_attn_fp8 launch");
   if (st != CW_OK || num_splits == 1) return st;
-  if (head_dim == 128)
-    hipLaunchKernelGGL(decode_join_kernel<128>, dim3(unsigned(rows)), dim3(kThreads), 0, s, a.part_o, a.part_lse,
-                       num_splits, rows, a.out);
-  else
-    hipLaunchKernelGGL(decode_join_kernel<64>, dim3(unsigned(rows)), dim3(kThreads), 0, s, a.part_o, a.part_lse,
-                       num_splits, rows, a.out);
-  return check_launch("decode_attn_fp8 join launch");
+  return cw::decode_join("decode_attn_fp8", head_dim, a.part_o, a.part_lse, num_splits, rows, out, stream);
 }

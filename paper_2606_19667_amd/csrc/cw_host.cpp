@@ -73,6 +73,20 @@ cw_status check_cache_fp8(const char* what, const void* k8, const void* v8, cons
   return CW_OK;
 }
 
+cw_status check_cache_fp4(const char* what, const void* pages, const int32_t* block_table, int32_t num_kv_heads,
+                          int32_t head_dim, int32_t block_size, int32_t num_blocks) {
+  const std::string w(what);
+  if (!pages || !block_table) return fail(CW_EINVAL, w + ": a required pointer is NULL");
+  if (num_kv_heads < 1) return fail(CW_EINVAL, w + ": num_kv_heads must be >= 1");
+  if (num_blocks < 1) return fail(CW_EINVAL, w + ": num_blocks must be >= 1");
+  if (head_dim != 64 && head_dim != 128) return fail(CW_EUNSUPPORTED, w + ": head_dim must be 64 or 128");
+  if (block_size != kBlockSize) return fail(CW_EUNSUPPORTED, w + ": block_size must be 16");
+  if (num_kv_heads > kMaxKvHeads) return fail(CW_EUNSUPPORTED, w + ": more than 65536 KV heads");
+  if ((reinterpret_cast<uintptr_t>(pages) & 15) != 0)
+    return fail(CW_EINVAL, w + ": the pages must be 16-byte aligned");
+  return CW_OK;
+}
+
 int64_t count_tiles(const int32_t* cu, int32_t batch, int32_t hkv, int32_t per_tile) {
   int64_t n = 0;
   for (int32_t r = 0; r < batch; ++r) n += (int64_t(cu[r + 1] - cu[r]) + per_tile - 1) / per_tile;

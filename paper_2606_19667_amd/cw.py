@@ -109,6 +109,17 @@ def _load() -> ctypes.CDLL:
         "cw_decode_attn_fp8_workspace_bytes": (_i64, [_i32, _i32, _i32, _i32]),
         "cw_decode_attn_fp8": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
                                       _f32, _i32, _vp, _i64, _vp, _vp]),
+        "cw_rope_append_fp4": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _vp,
+                                      _vp, _pi32, _pi32, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
+        "cw_cache_rows_fp4": (_i32, [_vp, _vp, _i32, _vp, _vp, _pi32, _pi32, _i32, _i32, _i32, _i32, _i32, _vp, _vp,
+                                     _vp]),
+        "cw_suffix_prefill_attn_fp4": (_i32, [_vp, _vp, _vp, _i32, _pi32, _pi32, _i32, _i32, _i32, _i32, _i32, _i32,
+                                              _f32, _pi32, _vp, _vp, _vp]),
+        "cw_suffix_prefill_attn_split_fp4": (_i32, [_vp, _vp, _vp, _i32, _pi32, _pi32, _i32, _i32, _i32, _i32, _i32,
+                                                    _i32, _f32, _pi32, _vp, _vp, _i64, _vp, _vp]),
+        "cw_decode_attn_fp4_workspace_bytes": (_i64, [_i32, _i32, _i32, _i32]),
+        "cw_decode_attn_fp4": (_i32, [_vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _i32, _vp,
+                                      _i64, _vp, _vp]),
         "cw_probe_mfma_bf16_flops": (_i64, [_i32, _i32]),
         "cw_probe_mfma_bf16": (_i32, [_vp, _i64, _vp, _i32, _i32, _vp]),
     }
@@ -134,6 +145,8 @@ EXPORTED = ("cw_abi_version", "cw_last_error", "cw_block_hashes", "cw_pool_creat
             "cw_add_rms_norm_fp8", "cw_fp8_linear", "cw_rope_append_fp8", "cw_suffix_prefill_attn_fp8",
             "cw_suffix_prefill_attn_split_fp8",
             "cw_decode_attn_fp8_workspace_bytes", "cw_decode_attn_fp8",
+            "cw_rope_append_fp4", "cw_cache_rows_fp4", "cw_suffix_prefill_attn_fp4",
+            "cw_suffix_prefill_attn_split_fp4", "cw_decode_attn_fp4_workspace_bytes", "cw_decode_attn_fp4",
             "cw_probe_mfma_bf16_flops", "cw_probe_mfma_bf16")
 
 
@@ -1061,6 +1074,225 @@ def decode_attn_fp8(q: torch.Tensor, cache: Fp8KvCache, block_table: torch.Tenso
     _check(_lib.cw_decode_attn_fp8(
         _arg(q, bf16, "q", dev), *cache._args(hkv, D, dev), _arg(block_table, i32, "block_table", dev), stride,
         _arg(seq_lens, i32, "seq_lens", dev), B, hq, hkv, D, BLOCK_SIZE, cache.k.shape[0], softmax_scale, num_splits,
+        None if workspace is None else _arg(workspace, torch.uint8, "workspace", dev),
+        0 if workspace is None else workspace.numel(), _arg(out, bf16, "out", dev), _stream_of(stream, dev)))
+    return out
+
+
+# ---------------------------------------------------------------- the 4-bit cache
+class Fp4KvCache:
+    """A 4-bit paged KV cache: pages uint8 [num_blocks, Hkv, 17 D], each the codes
+    (e2m1) and scales of one (block of 16 tokens, KV head) as cw.h lays them out. D
+    is 64 or 128. What no append has written is whatever the memory held."""
+
+    def __init__(self, num_blocks: int, num_kv_heads: int, head_dim: int, device="cuda"):
+        self.pages = torch.empty((int(num_blocks), int(num_kv_heads), 17 * int(head_dim)), dtype=torch.uint8,
+                                 device=device)
+
+    @classmethod
+    def of(cls, pages: torch.Tensor) -> "Fp4KvCache":
+        """The cache held in the given tensor (not copied)."""
+        if pages.dim() != 3 or pages.shape[2] not in (17 * 64, 17 * 128):
+            raise ValueError("pages must be [num_blocks, Hkv, 17 * D] with D 64 or 128")
+        self = cls.__new__(cls)
+        self.pages = pages
+        return self
+
+    @property
+    def num_blocks(self) -> int:
+        return int(self.pages.shape[0])
+
+    @property
+    def num_kv_heads(self) -> int:
+        return int(self.pages.shape[1])
+
+    @property
+    def head_dim(self) -> int:
+        return int(self.pages.shape[2]) // 17
+
+    def _arg(self, num_kv_heads: int, head_dim: int, dev: int) -> int:
+        if self.pages.shape[1:] != (num_kv_heads, 17 * head_dim):
+            raise ValueError(f"the cache holds {self.num_kv_heads} KV heads of {self.head_dim}, "
+                             f"the call has {num_kv_heads} of {head_dim}")
+        return _arg(self.pages, torch.uint8, "cache.pages", dev)
+
+
+def rope_append_fp4(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp4KvCache,
+                    q: torch.Tensor | None = None, rope: torch.Tensor | None = None, interleaved: bool = False,
+                    q_out: torch.Tensor | None = None, stream=None) -> torch.Tensor | None:
+    """cw_rope_append_fp4: rotate the suffix rows' q [total_s, Hq, D] and k
+    [total_s, Hkv, D] with the table rope [n, pairs, 2] (the first 2 * pairs
+    columns of a head; interleaved: neighbouring columns are a pair, else the
+    halves of them) and write k and v to the 4-bit cache; the rows of q, k and v
+    may lie apart (slices of one projection). Returns q_out [total_s, Hq, D] bf16
+    (None without q). Without rope (and q) keys are stored as they are. The prefix
+    lengths of meta may be any."""
+    if DEBUG_CHECK_COPIES:
+        meta.check_device_copies()
+    hq, hkv, D, T = meta.num_q_heads, meta.num_kv_heads, meta.head_dim, int(meta.cu_host[-1])
+    for name, t, h in (("q", q, hq), ("k", k, hkv), ("v", v, hkv)):
+        if t is not None and t.shape != (T, h, D):
+            raise ValueError(f"{name} must be [{T}, {h}, {D}], got {tuple(t.shape)}")
+    if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2):
+        raise ValueError(f"rope must be [n, pairs, 2], got {tuple(rope.shape)}")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    if q is not None and q_out is None:
+        q_out = _new(stream, (T, hq, D), torch.bfloat16, q.device)
+    elif q_out is not None and q_out.shape != (T, hq, D):
+        raise ValueError(f"q_out must be [{T}, {hq}, {D}]")
+    dev, bf16, i32 = _device(cache.pages, "cache.pages"), torch.bfloat16, torch.int32
+    pk, sk = _rows(k, bf16, "k", dev)
+    pv, sv = _rows(v, bf16, "v", dev)
+    pq, sq = (None, 0) if q is None else _rows(q, bf16, "q", dev)
+    _check(_lib.cw_rope_append_fp4(
+        pq, sq, pk, sk, pv, sv, None if rope is None else _arg(rope, torch.float32, "rope", dev),
+        0 if rope is None else rope.shape[0], 0 if rope is None else 2 * rope.shape[1], 1 if interleaved else 0,
+        None if q_out is None else _arg(q_out, bf16, "q_out", dev), cache._arg(hkv, D, dev),
+        _arg(meta.bt, i32, "block_table", dev), meta.bt_stride, _arg(meta.cu, i32, "cu_suffix", dev),
+        _arg(meta.plen, i32, "prefix_len", dev), meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv,
+        D, BLOCK_SIZE, cache.num_blocks, _stream_of(stream, dev)))
+    return q_out
+
+
+def cache_rows_fp4(meta: BatchMeta, cache: Fp4KvCache, k_rows: torch.Tensor | None = None,
+                   v_rows: torch.Tensor | None = None, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """cw_cache_rows_fp4: the keys and values of the suffix rows of `meta` as the
+    4-bit cache holds them, (k_rows, v_rows) bf16 [total_s, Hkv, D]. (A prefix is
+    the suffix of a description whose prefix lengths are zero.)"""
+    if DEBUG_CHECK_COPIES:
+        meta.check_device_copies()
+    hkv, D = meta.num_kv_heads, meta.head_dim
+    shape = (meta.total_rows, hkv, D)
+    dev, bf16, i32 = _device(cache.pages, "cache.pages"), torch.bfloat16, torch.int32
+    if k_rows is None:
+        k_rows = _new(stream, shape, bf16, cache.pages.device)
+    if v_rows is None:
+        v_rows = _new(stream, shape, bf16, cache.pages.device)
+    for name, t in (("k_rows", k_rows), ("v_rows", v_rows)):
+        if t.shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}, got {tuple(t.shape)}")
+    _check(_lib.cw_cache_rows_fp4(
+        cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
+        _arg(meta.cu, i32, "cu_suffix", dev), _arg(meta.plen, i32, "prefix_len", dev), meta._hp(meta.cu_host),
+        meta._hp(meta.plen_host), meta.batch, hkv, D, BLOCK_SIZE, cache.num_blocks, _arg(k_rows, bf16, "k_rows", dev),
+        _arg(v_rows, bf16, "v_rows", dev), _stream_of(stream, dev)))
+    return k_rows, v_rows
+
+
+def suffix_prefill_attn_fp4(meta: BatchMeta, q: torch.Tensor, cache: Fp4KvCache, softmax_scale: float,
+                            out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """cw_suffix_prefill_attn_fp4: attention of the suffix rows over the 4-bit
+    cache; returns out [total_s, Hq, D] bf16. The prefix lengths of meta may be any.
+    Keys are not cut into runs: a caller with few rows behind long prefixes takes
+    suffix_prefill_attn_split_fp4, whose default count comes back here where runs
+    do not pay."""
+    if DEBUG_CHECK_COPIES:
+        meta.check_device_copies()
+    hq, hkv, D = meta.num_q_heads, meta.num_kv_heads, meta.head_dim
+    if q.shape != (meta.total_rows, hq, D):
+        raise ValueError(f"q must be [{meta.total_rows}, {hq}, {D}], got {tuple(q.shape)}")
+    if out is None:
+        out = _new(stream, q.shape, torch.bfloat16, q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
+    _check(_lib.cw_suffix_prefill_attn_fp4(
+        _arg(q, bf16, "q", dev), cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
+        meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.num_blocks,
+        softmax_scale, meta._hp(meta.plan_host), _arg(meta.plan, i32, "plan", dev), _arg(out, bf16, "out", dev),
+        _stream_of(stream, dev)))
+    return out
+
+
+def split_count_fp4(meta: BatchMeta) -> int:
+    """A split count for cw_suffix_prefill_attn_split_fp4: split_count's, with runs of 512
+    keys at least."""
+    longest = int((meta.plen_host + np.diff(meta.cu_host)).max())
+    return max(1, min(split_count(meta), longest // 512))
+
+
+def suffix_prefill_attn_split_fp4(meta: BatchMeta, q: torch.Tensor, cache: Fp4KvCache, softmax_scale: float,
+                                  num_splits: int | None = None, workspace: torch.Tensor | None = None,
+                                  out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """cw_suffix_prefill_attn_split_fp4: suffix_prefill_attn_fp4 with each tile's keys in
+    num_splits runs (by default split_count_fp4's; without runs the call is
+    suffix_prefill_attn_fp4), for few rows behind long prefixes.
+    `workspace` (uint8, device) is allocated when not given; calls that may run
+    at the same time, captured ones among them, need one each."""
+    if DEBUG_CHECK_COPIES:
+        meta.check_device_copies()
+    hq, hkv, D = meta.num_q_heads, meta.num_kv_heads, meta.head_dim
+    if q.shape != (meta.total_rows, hq, D):
+        raise ValueError(f"q must be [{meta.total_rows}, {hq}, {D}], got {tuple(q.shape)}")
+    if out is None:
+        out = _new(stream, q.shape, torch.bfloat16, q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if num_splits is None:
+        num_splits = split_count_fp4(meta)
+        if num_splits == 1:
+            return suffix_prefill_attn_fp4(meta, q, cache, softmax_scale, out, stream)
+    need = split_workspace_bytes(meta, num_splits)
+    if workspace is None:
+        workspace = _new(stream, max(need, 1), torch.uint8, q.device)
+    plan_host, plan_dev = meta.split_plan(int(num_splits))
+    dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
+    _check(_lib.cw_suffix_prefill_attn_split_fp4(
+        _arg(q, bf16, "q", dev), cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
+        meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.num_blocks,
+        softmax_scale, meta._hp(plan_host), _arg(plan_dev, i32, "plan", dev),
+        _arg(workspace, torch.uint8, "workspace", dev), workspace.numel(), _arg(out, bf16, "out", dev),
+        _stream_of(stream, dev)))
+    return out
+
+
+def decode_split_count_fp4(batch: int, num_q_heads: int, num_kv_heads: int, max_len: int) -> int:
+    """A split count for cw_decode_attn_fp4 with sequences of up to max_len tokens."""
+    tiles = max(1, int(batch) * int(num_kv_heads) * -(-int(num_q_heads) // (16 * int(num_kv_heads))))
+    return max(1, min(64, max(-(-768 // tiles), int(max_len) // 1500), int(max_len) // 256))
+
+
+def decode_workspace_bytes_fp4(batch: int, num_q_heads: int, head_dim: int, num_splits: int) -> int:
+    n = int(_lib.cw_decode_attn_fp4_workspace_bytes(int(batch), int(num_q_heads), int(head_dim), int(num_splits)))
+    if n < 0:
+        _check(n)
+    return n
+
+
+def decode_attn_fp4(q: torch.Tensor, cache: Fp4KvCache, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                    softmax_scale: float, num_splits: int | None = None, workspace: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """cw_decode_attn_fp4: one query row per request, q [batch, Hq, D] bf16, over
+    the first seq_lens [batch] (int32, device) tokens of its row of block_table
+    [batch, stride] (int32, device); returns out [batch, Hq, D] bf16. `workspace`
+    (uint8, device) is allocated when not given; calls that may run at the same
+    time, captured ones among them, need one each. What a call of this section
+    allocates belongs to its stream."""
+    if q.dim() != 3:
+        raise ValueError(f"q must be [batch, Hq, D], got {tuple(q.shape)}")
+    B, hq, D = q.shape
+    hkv = cache.num_kv_heads
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"block_table must be [{B}, stride], got {tuple(block_table.shape)}")
+    if seq_lens.shape != (B,):
+        raise ValueError(f"seq_lens must be [{B}], got {tuple(seq_lens.shape)}")
+    if out is None:
+        out = _new(stream, q.shape, torch.bfloat16, q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    stride = int(block_table.shape[1])
+    if hkv < 1:
+        raise ValueError("the cache has no KV heads")
+    if num_splits is None:
+        num_splits = decode_split_count_fp4(B, hq, hkv, stride * BLOCK_SIZE)
+    need = decode_workspace_bytes_fp4(B, hq, D, num_splits)
+    if workspace is None and need:
+        workspace = _new(stream, need, torch.uint8, q.device)
+    dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
+    _check(_lib.cw_decode_attn_fp4(
+        _arg(q, bf16, "q", dev), cache._arg(hkv, D, dev), _arg(block_table, i32, "block_table", dev), stride,
+        _arg(seq_lens, i32, "seq_lens", dev), B, hq, hkv, D, BLOCK_SIZE, cache.num_blocks, softmax_scale, num_splits,
         None if workspace is None else _arg(workspace, torch.uint8, "workspace", dev),
         0 if workspace is None else workspace.numel(), _arg(out, bf16, "out", dev), _stream_of(stream, dev)))
     return out
