@@ -32,6 +32,8 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int64_t kMaxGrid = UINT32_MAX / kThreads;   // a launch has fewer than 2^32 threads along an axis
 
+typedef const __attribute__((address_space(4))) int32_t cint32_t;
+
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
@@ -387,8 +389,8 @@ __global__ __launch_bounds__(kThreads) void cache_rows_fp4_kernel(const RowsArgs
 // A workgroup takes (request, KV head, up to 16 query heads of its group, run of 32-key chunks);
 // each of its waves takes a part of the run, with a softmax state of its own, and they join their
 // states at the end. Reading the cache once bounds it. A wave reads pages straight into registers
-// in the operand layout of v_mfma_f32_16x16x32_bf16, a page in four instructions, kAhead chunks
-// ahead; nothing passes through LDS:
+// in the operand layout of v_mfma_f32_16x16x32_bf16, a page in four instructions, a chunk ahead;
+// nothing passes through LDS:
 //  * S^T = K Q^T. Lane (c, u) = (l % 16, l / 16) holds of key c the columns u D / 4 .. + D / 4 - 1,
 //    consecutive bytes with one scale (the order of the columns is the same for Q). Its
 //    accumulators are the scores of the keys 4 u .. 4 u + 3 of a block for query column c.
@@ -400,6 +402,24 @@ __global__ __launch_bounds__(kThreads) void cache_rows_fp4_kernel(const RowsArgs
 // The base of a column's exponents is the row maximum of the wave's first chunk and moves only when
 // a sum passes 2^30 (bf16 and fp32 have the range), so later chunks need no maximum. The row's sum
 // takes the probabilities as they are rounded for the product.
+// HBM-bound when sequences are long: 64 requests of about 10,367 tokens, 64 / 8 heads of 128 (720 MB) 136 us, 5.3 TB/s
+// (a copy 4.8 to 5.3). Of few chunks it is bound by the chain of length, table word, codes, scores, softmax, product
+// and join (4.2 us for 300 tokens of 4 heads of 64), and by a wave's instructions: a chunk is 146 vector ones, 64 of
+// them conversions and 32 permutes, and takes a lone wave 0.7 us whether one, two or three chunks are in flight ahead.
+// More waves a workgroup (8, 12, 16) in place of runs: 16 x 1,407 tokens 12.6, 12.2, 12.0 against 12.0, 1 x 9,000 34 to
+// 37 against 8.7.
+// n / d for n < 2^31 by a multiplication: a division in software is 25 instructions, and a workgroup with few
+// chunks has several ahead of its first load.
+struct FastDiv {
+  uint32_t mul, shift, d;
+  explicit FastDiv(uint32_t by = 1) : shift(0), d(by) {
+    while ((uint64_t(1) << shift) < by) ++shift;
+    mul = uint32_t(((uint64_t(1) << (31 + shift)) + by - 1) / by);
+    shift += 31;
+  }
+  __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return uint32_t((uint64_t(n) * mul) >> shift); }
+};
+
 struct DecodeArgs {
   const uint16_t* q;
   const uint8_t* pages;
@@ -408,39 +428,51 @@ struct DecodeArgs {
   uint16_t* out;      // splits == 1
   float* part_o;      // else fp32 [splits][batch * hq][D], normalised
   float* part_lse;    // and base-2 log-sum-exp [splits][batch * hq]
-  int bt_stride, batch, hq, hkv, group, num_blocks, splits, head_tiles;
+  int bt_stride, batch, hq, hkv, group, num_blocks, splits;
+  FastDiv by_splits, by_tiles, by_heads;   // division by splits, by the head tiles of a group, by hkv
   float c_log2;
 };
 
 constexpr int kChunk = 32;      // keys of a wave's step: two blocks
 constexpr int kTileHeads = 16;
-constexpr int kAhead = 2;       // chunks in flight ahead of the one that a wave works on
 constexpr float kMaxSum = 0x1p30f;
 
-template <int D>
-__global__ __launch_bounds__(kThreads) void decode_attn_fp4_kernel(const DecodeArgs a) {
+constexpr int kAhead = 1;       // chunks in flight ahead of the one that a wave works on
+constexpr int kRawBuffer = 0x00027000;   // a buffer's last word: bytes at offsets, checked against its size
+
+template <int D, bool ONCE>
+__device__ __forceinline__ typename Piece<D>::Lane load_lane(__amdgpu_buffer_rsrc_t page, int offset) {
+  constexpr int AUX = ONCE ? 2 : 0;   // non-temporal
+  if constexpr (D == 128) return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(page, offset, 0, AUX));
+  else return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(page, offset, 0, AUX));
+}
+
+// ONCE: the codes are read past the caches' order of use.
+template <int D, bool ONCE>
+__global__ __launch_bounds__(kThreads, 3) void decode_attn_fp4_kernel(const DecodeArgs a) {
   constexpr int KS = D / 32;          // MFMA k-steps over D
   constexpr int DT = D / 16;          // output tiles over D, and columns of a lane's piece
-  constexpr int NW = D / 32;          // words of codes a lane holds of a page's keys, and of its values
   using Lane = typename Piece<D>::Lane;
   __shared__ __attribute__((aligned(16))) float s_o[kWaves][kTileHeads][D];
   __shared__ float s_m[kWaves][kTileHeads], s_l[kWaves][kTileHeads];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, u = lane >> 4;
-  int w = blockIdx.x;
-  const int split = w % a.splits;
-  w /= a.splits;
-  const int ht = w % a.head_tiles;
-  w /= a.head_tiles;
-  const int g = w % a.hkv, b = w / a.hkv;
+  uint32_t w = a.by_splits.quotient(blockIdx.x);
+  const int split = int(blockIdx.x - w * a.by_splits.d);
+  uint32_t x = a.by_tiles.quotient(w);
+  const int ht = int(w - x * a.by_tiles.d);
+  const int b = int(a.by_heads.quotient(x));
+  const int g = int(x - uint32_t(b) * a.by_heads.d);
+  const int seq = reinterpret_cast<cint32_t*>(reinterpret_cast<uintptr_t>(a.seq_lens))[b];
   const int head0 = g * a.group + ht * kTileHeads;
   const int nheads = min(kTileHeads, a.group - ht * kTileHeads);
-  const int len = int(min(int64_t(max(a.seq_lens[b], 0)), int64_t(a.bt_stride) * kBs));
+  const int len = min(max(seq, 0), a.bt_stride * kBs);   // (the host keeps bt_stride below 2^27 - 256)
   const int chunks = (len + kChunk - 1) / kChunk;
-  const int c_begin = int(int64_t(chunks) * split / a.splits), c_end = int(int64_t(chunks) * (split + 1) / a.splits);
-  const int w_begin = c_begin + (c_end - c_begin) * wave / kWaves;
-  const int w_end = c_begin + (c_end - c_begin) * (wave + 1) / kWaves;
+  // runs and parts of runs differ by one chunk at most
+  const int per = int(a.by_splits.quotient(uint32_t(chunks))), over = chunks - per * a.splits;
+  const int c_begin = per * split + min(split, over), c_len = per + (split < over ? 1 : 0);
+  const int w_begin = c_begin + c_len * wave / kWaves, w_end = c_begin + c_len * (wave + 1) / kWaves;
   const int32_t* const bt = a.bt + int64_t(b) * a.bt_stride;
   const int last_block = (len + kBs - 1) / kBs - 1;   // (-1 for an empty request, which has no chunk)
 
@@ -463,19 +495,16 @@ __global__ __launch_bounds__(kThreads) void decode_attn_fp4_kernel(const DecodeA
   };
   const uint8_t* const pages = a.pages + int64_t(g) * kPage<D>;
   const int64_t block_bytes = int64_t(a.hkv) * kPage<D>;
-  // Table words, 64 blocks (32 chunks) at a time, block i's in lane i: -1 past the sequence or
-  // outside the pool, whose keys and values are zeros.
+  // Table words, 64 blocks (32 chunks) at a time, block i's in lane i.
   auto words = [&](int chunk) __attribute__((always_inline)) -> int {
-    const int lb = chunk * 2 + lane;
-    const int id = bt[min(lb, max(last_block, 0))];
-    return lb <= last_block && id >= 0 && id < a.num_blocks ? id : -1;
+    return bt[min(chunk * 2 + lane, max(last_block, 0))];
   };
   int ids = -1, ids_next = -1, ids_at = w_begin;   // of the chunks ids_at .. + 31, and of the 32 after them
   if (w_begin < w_end) {
     ids = words(w_begin);
-    ids_next = words(w_begin + 32);
+    if (w_end - w_begin > 32) ids_next = words(w_begin + 32);
   }
-  const int ko = col * (D / 2) + u * (D / 8);
+  const int ko = col * (D / 2) + u * (D / 8), vo = kValues<D> + lane * (D / 8);
   const int kso = kKeyScales<D> + col * (D / 32) + u * (D / 4) / 32;
   const int vso = kValueScales<D> + col * DT / 32 * kBs + 4 * u;
   auto load = [&](Chunk& x, int chunk) __attribute__((always_inline)) {
@@ -486,16 +515,15 @@ __global__ __launch_bounds__(kThreads) void decode_attn_fp4_kernel(const DecodeA
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int id = __builtin_amdgcn_readlane(ids, (chunk - ids_at) * 2 + i);
-      const uint8_t* const page = pages + int64_t(max(id, 0)) * block_bytes;
-      x.k[i] = *reinterpret_cast<const Lane*>(page + uint32_t(ko));
-      x.v[i] = *reinterpret_cast<const Lane*>(page + kValues<D> + uint32_t(lane) * (D / 8));
-      x.ks[i] = page[uint32_t(kso)];
-      x.vs[i] = *reinterpret_cast<const uint32_t*>(page + uint32_t(vso));
-      if (__builtin_expect(id < 0, 0)) {
-        x.k[i] = x.v[i] = Lane{};
-        x.ks[i] = x.vs[i] = 0;
-      }
+      // (past the sequence, or outside the pool: a buffer of no bytes, whose loads give zeros)
+      const int id = __builtin_amdgcn_readlane(ids, __builtin_amdgcn_readfirstlane((chunk - ids_at) * 2 + i));
+      const bool ok = chunk * 2 + i <= last_block && uint32_t(id) < uint32_t(a.num_blocks);
+      const auto page = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pages + int64_t(ok ? id : 0) * block_bytes), 0,
+                                                          ok ? kPage<D> : 0, kRawBuffer);
+      x.k[i] = load_lane<D, ONCE>(page, ko);
+      x.v[i] = load_lane<D, ONCE>(page, vo);
+      x.ks[i] = __builtin_amdgcn_raw_buffer_load_b8(page, kso, 0, 0);
+      x.vs[i] = __builtin_amdgcn_raw_buffer_load_b32(page, vso, 0, 0);
     }
   };
 
@@ -518,6 +546,7 @@ __global__ __launch_bounds__(kThreads) void decode_attn_fp4_kernel(const DecodeA
         const u32x4 kf{widen<0>(c, ks), widen<1>(c, ks), widen<2>(c, ks), widen<3>(c, ks)};
         s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qf[st], s[i], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);   // (here and below: else conversions far ahead hold registers)
     }
     uint32_t vs[2] = {x.vs[0], x.vs[1]};
     if (__builtin_expect(left < kChunk, 0)) {
@@ -597,19 +626,19 @@ __global__ __launch_bounds__(kThreads) void decode_attn_fp4_kernel(const DecodeA
         }
       o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pf, o[j], 0, 0, 0);
       o[j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pf, o[j + 1], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
-  // Ring of kAhead + 1 chunks in registers (the loop is unrolled over it, so that each has its own).
-  constexpr int RING = kAhead + 1;
-  Chunk ring[RING];
+  // Chunks in flight, each in registers of its own: the loop is unrolled over them.
+  Chunk ring[kAhead + 1];
 #pragma unroll
   for (int i = 0; i < kAhead; ++i)
     if (w_begin + i < w_end) load(ring[i], w_begin + i);
   for (int chunk = w_begin; chunk < w_end;) {
 #pragma unroll
-    for (int i = 0; i < RING; ++i) {
-      if (chunk + kAhead < w_end) load(ring[(i + kAhead) % RING], chunk + kAhead);
+    for (int i = 0; i <= kAhead; ++i) {
+      if (chunk + kAhead < w_end) load(ring[(i + kAhead) % (kAhead + 1)], chunk + kAhead);
       work(ring[i], chunk);
       if (++chunk >= w_end) break;
     }
@@ -651,7 +680,7 @@ __global__ __launch_bounds__(kThreads) void decode_attn_fp4_kernel(const DecodeA
     } else {
       const int64_t at = int64_t(split) * a.batch * a.hq + row;
       *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = acc;
-      if (d == 0) a.part_lse[at] = c_begin < c_end ? M + __log2f(sum) : -INFINITY;
+      if (d == 0) a.part_lse[at] = c_len > 0 ? M + __log2f(sum) : -INFINITY;
     }
   }
 }
@@ -842,12 +871,19 @@ extern "C" cw_status cw_decode_attn_fp4(const void* q, const void* pages, const 
   a.group = num_q_heads / num_kv_heads;
   a.num_blocks = num_blocks;
   a.splits = num_splits;
-  a.head_tiles = (a.group + kTileHeads - 1) / kTileHeads;
+  const int head_tiles = (a.group + kTileHeads - 1) / kTileHeads;
+  a.by_splits = FastDiv(num_splits);
+  a.by_tiles = FastDiv(head_tiles);
+  a.by_heads = FastDiv(num_kv_heads);
   a.c_log2 = softmax_scale * 1.4426950408889634f;
-  const int64_t grid = int64_t(batch) * num_kv_heads * a.head_tiles * num_splits;
+  const int64_t grid = int64_t(batch) * num_kv_heads * head_tiles * num_splits;
   if (grid > kMaxGrid || rows > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
   auto* const s = static_cast<hipStream_t>(stream);
-  auto* const kernel = head_dim == 128 ? decode_attn_fp4_kernel<128> : decode_attn_fp4_kernel<64>;
+  // A cache that the last-level cache (256 MiB) cannot hold is read past it. us, 64 requests of about 10,367 tokens,
+  // 720 MB: 138 against 153; 8 heads of 9,000 tokens, 10 MB, read again and again: 60 against 55.
+  const bool once = int64_t(batch) * bt_stride * num_kv_heads * 17 * head_dim > (int64_t(256) << 20);
+  auto* const kernel = head_dim == 128 ? (once ? decode_attn_fp4_kernel<128, true> : decode_attn_fp4_kernel<128, false>)
+                                       : (once ? decode_attn_fp4_kernel<64, true> : decode_attn_fp4_kernel<64, false>);
   hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(kThreads), 0, s, a);
   st = check_launch("decode_attn_fp4 launch");
   if (st != CW_OK || num_splits == 1) return st;
