@@ -20,6 +20,7 @@
 #include <cmath>
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "cw_fp4.h"
 #include "cw_internal.h"
@@ -96,15 +97,20 @@ __device__ __forceinline__ Unit find_unit(const int32_t* cu, const int32_t* plen
 // ---------------------------------------------------------------------------
 // Append: rotary embedding, then 4-bit codes and scales.
 //
-// A wave takes one (block, head) at a time: lane l holds the columns D / 16 (l % 16) .. of the
-// tokens 4 (l / 16) .. + 3, which are the D / 8 bytes that it stores of a value page. A rotation's
-// other column is in the same lane (neighbours) or in another of the 16 (halves). Each group of 32
-// columns lies in 512 / D neighbouring lanes.
+// A wave takes one (four tokens of a block, head) at a time: lane l holds the columns D / 16 (l % 16) ..
+// of token l / 16 of the four, so loads and stores are whole rows, of value pages too. A rotation's other
+// column is in the same lane (neighbours) or in another of the 16 (halves). Each group of 32 columns lies
+// in 512 / D neighbouring lanes. The wave keeps its tokens' cosines and sines over all its heads, and has the
+// rows of four heads in flight at once.
 //
 // A value next to a border of two codes has to fall on its side of it, so keys are rotated by the
 // difference of two products without cancellation error (t = w s; d = x c - t; d - (w s - t), at
 // most 1.5 units off in the last place), and a wave that holds a value within 4 such units of a
 // border (they all have a mantissa of 2 bits) rotates again in 64 bits: few waves do.
+// HBM-bound: reads 2 (Hq + 2 Hkv) D bytes a row, writes 2 Hq D + 17/16 Hkv D. 16,128 rows of 32 / 8 heads of 128:
+// 72 us, 4.8 TB/s (a copy 4.8 to 5.3); 64 requests of one row 4.7 us in a captured graph, 18 called one by one
+// with a split of the projection's rows and the read, which is the host's time. A wave with 16 tokens of a head at a
+// time, whose 64-bit form took 250 registers: 89 and 9.6; one row in flight 130; a wait for stores before each head 103.
 struct AppendArgs {
   const uint16_t* q;
   const uint16_t* k;
@@ -140,6 +146,7 @@ __device__ __forceinline__ float turned(float x, float w, float c, float s) {
 // The same with its last bit set where it is not exact: rounded on to fewer bits it goes where the
 // exact value goes, as it is never halfway by rounding alone.
 __device__ __forceinline__ float turned_to_odd(float x, float w, float c, float s) {
+  asm volatile("" : "+v"(c), "+v"(s));   // (else the table is converted ahead of the loop over heads, in 32 registers)
   const double y = fma(double(x), double(c), -(double(w) * double(s)));
   const float v = float(y);
   const double rest = y - double(v);
@@ -148,11 +155,12 @@ __device__ __forceinline__ float turned_to_odd(float x, float w, float c, float 
   return __uint_as_float((rest > 0.) == (v > 0.f) ? b + 1 : b - 1);
 }
 
-// HALVES: column j is paired with j + pairs; else 2 j with 2 j + 1.
-template <int D, bool HALVES>
+// HALVES: column j is paired with j + pairs; else 2 j with 2 j + 1. ONCE: rows in and queries out pass the caches'
+// order of use.
+template <int D, bool HALVES, bool ONCE>
 __global__ __launch_bounds__(kThreads) void rope_append_fp4_kernel(const AppendArgs a) {
   constexpr int PC = D / 16;    // columns a lane holds
-  constexpr int NT = HALVES ? PC : PC / 2;   // (cos, sin) pairs a lane needs of a token
+  constexpr int NT = HALVES ? PC : PC / 2;   // (cos, sin) pairs a lane needs
   using Words = typename Piece<D>::Bf16;     // PC bfloat16 values
   __shared__ int s_unit[2];
   const Unit un = find_unit(a.cu, a.plen, a.batch, s_unit);
@@ -162,172 +170,140 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp4_kernel(const AppendA
   const bool in_pool = blk >= 0 && blk < a.num_blocks;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int p = lane & 15, t0 = un.first + 4 * (lane >> 4), col = p * PC;
-  bool live[4];
-  int64_t row[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    live[i] = t0 + i >= un.begin && t0 + i < un.end;
-    row[i] = un.row0 + ((live[i] ? t0 + i : un.begin) - un.P);
-  }
-  const bool all = live[0] && live[3];
-
+  const int p = lane & 15, u = lane >> 4, col = p * PC;
   const bool turns = a.rope != nullptr && col < 2 * a.pairs;   // this lane's columns are rotated
   const bool upper = HALVES && col >= a.pairs;
   const int partner = (lane & 48) | (turns && HALVES ? (upper ? col - a.pairs : col + a.pairs) / PC : p);
-  const bool far8 = HALVES && a.pairs == D / 2;   // (the same for all lanes)
-  float cs[4][NT], sn[4][NT];
-  if (a.rope) {
-    const int j0 = HALVES ? (upper ? col - a.pairs : col) : col / 2;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int pos = min(live[i] ? t0 + i : un.begin, a.rope_len - 1);
-      const f32x4* src = reinterpret_cast<const f32x4*>(a.rope + int64_t(pos) * a.pairs + (turns ? j0 : 0));
-#pragma unroll
-      for (int n = 0; n < NT / 2; ++n) {
-        const f32x4 two = src[n];
-        cs[i][2 * n] = two[0];
-        sn[i][2 * n] = upper ? -two[1] : two[1];
-        cs[i][2 * n + 1] = two[2];
-        sn[i][2 * n + 1] = upper ? -two[3] : two[3];
-      }
-    }
-  }
+  const bool far8 = a.pairs == D / 2;   // halves of the whole head: the partner is lane ^ 8 of the 16
+  const int j0 = !turns ? 0 : HALVES ? (upper ? col - a.pairs : col) : col / 2;
+  const bool first_of_group = (p & (512 / D - 1)) == 0;
+  const int grp = p / (512 / D);
 
-  const int heads = a.hq + 2 * a.hkv;
-  const int step = int(gridDim.y) * kWaves;
-  Words raw[4];
-  auto load = [&](int h) __attribute__((always_inline)) {
+  // The four waves share the fours of tokens that have rows, and where these are fewer than three the heads.
+  const int i_begin = (un.begin - un.first) / 4, fours = (un.end - un.first + 3) / 4 - i_begin;
+  const int share = fours >= 3 ? 1 : fours == 2 ? 2 : 4;   // waves of a four
+  const int i = i_begin + wave / share;
+  if (i >= i_begin + fours) return;
+  const int heads = a.hq + 2 * a.hkv, step = int(gridDim.y) * share, h0 = int(blockIdx.y) * share + wave % share;
+  const int t = un.first + 4 * i + u, slot = 4 * i + u;
+  const bool live = t >= un.begin && t < un.end;
+  const int64_t row = un.row0 + ((live ? t : un.begin) - un.P);
+  auto load = [&](int h) __attribute__((always_inline)) -> Words {
     const uint16_t* base = h < a.hq ? a.q + int64_t(h) * D
                            : h < a.hq + a.hkv ? a.k + int64_t(h - a.hq) * D
                                               : a.v + int64_t(h - a.hq - a.hkv) * D;
     const int64_t stride = h < a.hq ? a.q_stride : h < a.hq + a.hkv ? a.k_stride : a.v_stride;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      raw[i] = Words{};
-      if (live[i]) raw[i] = *reinterpret_cast<const Words*>(base + row[i] * stride + col);
+    Words x{};
+    if (live) {
+      const auto* const at = reinterpret_cast<const Words*>(base + row * stride + col);
+      x = ONCE ? __builtin_nontemporal_load(at) : *at;
     }
+    return x;
   };
-  int h = int(blockIdx.y) * kWaves + wave;
-  if (h < heads) load(h);
-  for (; h < heads; h += step) {
-    Words in[4];
+  float cs[NT], sn[NT];
+  if (a.rope) {
+    const f32x4* src = reinterpret_cast<const f32x4*>(a.rope + int64_t(min(live ? t : un.begin, a.rope_len - 1)) * a.pairs + j0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) in[i] = raw[i];
-    if (h + step < heads) load(h + step);
+    for (int n = 0; n < NT / 2; ++n) {
+      const f32x4 two = src[n];
+      cs[2 * n] = two[0];
+      sn[2 * n] = upper ? -two[1] : two[1];
+      cs[2 * n + 1] = two[2];
+      sn[2 * n + 1] = upper ? -two[3] : two[3];
+    }
+  }
+  auto work = [&](const Words in, int h) __attribute__((always_inline)) {
     const bool is_q = h < a.hq, is_v = h >= a.hq + a.hkv;
-    if (!is_q && !in_pool) continue;
-    float x[4][PC];
+    if (!is_q && !in_pool) return;
+    float x[PC];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < PC / 2; ++j) {
-        x[i][2 * j] = bf16_lo(in[i][j]);
-        x[i][2 * j + 1] = bf16_hi(in[i][j]);
-      }
+    for (int j = 0; j < PC / 2; ++j) {
+      x[2 * j] = bf16_lo(in[j]);
+      x[2 * j + 1] = bf16_hi(in[j]);
+    }
     if (a.rope && !is_v) {
-      Words other[4];
-      if (HALVES) {
+      Words other{};
+      if constexpr (HALVES) {
+        if (far8) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int j = 0; j < PC / 2; ++j) other[j] = dpp<0x128>(in[j]);
+        } else {
 #pragma unroll
-          for (int j = 0; j < PC / 2; ++j)
-            other[i][j] = far8 ? dpp<0x128>(in[i][j])   // lane ^ 8 of 16
-                               : uint32_t(__shfl(int(in[i][j]), partner));
+          for (int j = 0; j < PC / 2; ++j) other[j] = uint32_t(__shfl(int(in[j]), partner));
+        }
       }
-      bool near = false;
       auto turn_all = [&](auto turn) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < PC / 2; ++j) {
-            const float lo = bf16_lo(in[i][j]), hi = bf16_hi(in[i][j]);
-            float y0, y1;
-            if (HALVES) {
-              y0 = turn(lo, bf16_lo(other[i][j]), cs[i][2 * j % NT], sn[i][2 * j % NT]);
-              y1 = turn(hi, bf16_hi(other[i][j]), cs[i][(2 * j + 1) % NT], sn[i][(2 * j + 1) % NT]);
-            } else {
-              y0 = turn(lo, hi, cs[i][j % NT], sn[i][j % NT]);
-              y1 = turn(hi, lo, cs[i][j % NT], -sn[i][j % NT]);
-            }
-            x[i][2 * j] = turns ? y0 : lo;
-            x[i][2 * j + 1] = turns ? y1 : hi;
+        for (int j = 0; j < PC / 2; ++j) {
+          const float lo = bf16_lo(in[j]), hi = bf16_hi(in[j]);
+          float y0, y1;
+          if (HALVES) {
+            y0 = turn(lo, bf16_lo(other[j]), cs[2 * j % NT], sn[2 * j % NT]);
+            y1 = turn(hi, bf16_hi(other[j]), cs[(2 * j + 1) % NT], sn[(2 * j + 1) % NT]);
+          } else {
+            y0 = turn(lo, hi, cs[j % NT], sn[j % NT]);
+            y1 = turn(hi, lo, cs[j % NT], -sn[j % NT]);
           }
+          x[2 * j] = turns ? y0 : lo;
+          x[2 * j + 1] = turns ? y1 : hi;
+        }
       };
       turn_all(turned);
       if (!is_q) {
+        bool near = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < PC; ++j) {
-            const uint32_t b = __float_as_uint(x[i][j]);
-            near |= ((b + 4) & 0x1FFFFFu) <= 8 && x[i][j] != 0.f;
-          }
+        for (int j = 0; j < PC; ++j) near |= ((__float_as_uint(x[j]) + 4) & 0x1FFFFFu) <= 8 && x[j] != 0.f;
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(near && turns) != 0, 0)) turn_all(turned_to_odd);
       }
     }
     if (is_q) {
+      Words o;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        Words o;
-#pragma unroll
-        for (int j = 0; j < PC / 2; ++j) o[j] = pack_bf16x2(x[i][2 * j], x[i][2 * j + 1]);
-        if (live[i]) *reinterpret_cast<Words*>(a.q_out + (row[i] * a.hq + h) * D + col) = o;
+      for (int j = 0; j < PC / 2; ++j) o[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+      if (live) {
+        auto* const at = reinterpret_cast<Words*>(a.q_out + (row * a.hq + h) * D + col);
+        if constexpr (ONCE) __builtin_nontemporal_store(o, at);
+        else *at = o;
       }
-      continue;
+      return;
     }
     const int g = h - a.hq - (is_v ? a.hkv : 0);
     uint8_t* const page = a.pages + (int64_t(blk) * a.hkv + g) * kPage<D>;
-    uint32_t code[4], exp[4];
+    uint32_t top = 0;   // as an integer: an infinity or a NaN is above every finite value
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t top = 0;   // as an integer: an infinity or a NaN is above every finite value
-#pragma unroll
-      for (int j = 0; j < PC; ++j) top = max(top, __float_as_uint(x[i][j]) & 0x7FFFFFFFu);
-      top = group_max<D>(top);
-      // the smallest e with top <= 7 * 2^e: 7 = 1.75 * 2^2, and a mantissa above 1.75 carries
-      const int e = min(max(int((top + 0x1FFFFFu) >> 23) - 127 - 2, kMinExp), kMaxExp);
-      const bool bad = top >= 0x7F800000u;
-      exp[i] = bad ? 255u : uint32_t(e + 127);
-      code[i] = bad ? 0u : encode<PC>(x[i], __uint_as_float(uint32_t(e + 127) << 23));
+    for (int j = 0; j < PC; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+    top = group_max<D>(top);
+    // the smallest e with top <= 7 * 2^e: 7 = 1.75 * 2^2, and a mantissa above 1.75 carries
+    const int e = min(max(int((top + 0x1FFFFFu) >> 23) - 127 - 2, kMinExp), kMaxExp);
+    const bool bad = top >= 0x7F800000u;
+    const uint32_t exp = bad ? 255u : uint32_t(e + 127);
+    const uint32_t code = bad ? 0u : encode<PC>(x, __uint_as_float(uint32_t(e + 127) << 23));
+    if (live) {
+      const int at = is_v ? kValues<D> + ((i * 16 + p) * 4 + u) * (D / 32) : slot * (D / 2) + p * (D / 32);
+      *reinterpret_cast<typename Piece<D>::Code*>(page + at) = typename Piece<D>::Code(code);
+      if (first_of_group)
+        page[is_v ? kValueScales<D> + grp * kBs + slot : kKeyScales<D> + slot * (D / 32) + grp] = uint8_t(exp);
     }
-    const bool first_of_group = (p & (512 / D - 1)) == 0;
-    const int grp = p / (512 / D);
-    if (is_v) {
-      uint8_t* const dst = page + kValues<D> + lane * (D / 8);
-      uint8_t* const sdst = page + kValueScales<D> + grp * kBs + (t0 - un.first);
-      if (all) {
-        if constexpr (D == 128) *reinterpret_cast<u32x4*>(dst) = u32x4{code[0], code[1], code[2], code[3]};
-        else *reinterpret_cast<u32x2*>(dst) = u32x2{code[0] | code[1] << 16, code[2] | code[3] << 16};
-        if (first_of_group)
-          *reinterpret_cast<uint32_t*>(sdst) = exp[0] | exp[1] << 8 | exp[2] << 16 | exp[3] << 24;
-      } else {
+  };
+  constexpr int ROWS = 4;
+  constexpr int kAllLoaded = 0x0F70;   // vmcnt(0), no other counter
+  for (int h = h0; h < heads; h += ROWS * step) {
+    Words in[ROWS];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (live[i]) {
-            if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst + 4 * i) = code[i];
-            else *reinterpret_cast<uint16_t*>(dst + 2 * i) = uint16_t(code[i]);
-            if (first_of_group) sdst[i] = uint8_t(exp[i]);
-          }
-      }
-    } else {
+    for (int n = 0; n < ROWS; ++n)
+      if (h + n * step < heads) in[n] = load(h + n * step);
+    __builtin_amdgcn_s_waitcnt(kAllLoaded);   // (else every head's work begins with a wait for the stores before it)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (live[i]) {
-          const int slot = t0 - un.first + i;
-          uint8_t* const dst = page + slot * (D / 2) + p * (PC / 2);
-          if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst) = code[i];
-          else *reinterpret_cast<uint16_t*>(dst) = uint16_t(code[i]);
-          if (first_of_group) page[kKeyScales<D> + slot * (D / 32) + grp] = uint8_t(exp[i]);
-        }
-    }
+    for (int n = 0; n < ROWS; ++n)
+      if (h + n * step < heads) work(in[n], h + n * step);
   }
 }
 
 // ---------------------------------------------------------------------------
 // Rows of the cache as bf16. A wave takes one (block, head, keys or values): lane l converts the
 // columns D / 16 (l % 16) .. of four tokens, so that a store writes whole rows of four tokens.
-// HBM-bound by what it writes: 4 D bytes a token and head for 17 D / 16 read.
+// HBM-bound by what it writes, past the caches' order of use: 4 D bytes a token and head for 17 D / 16 read. 133,700
+// tokens of 8 heads of 128 (693 MB) 133 us, 5.2 TB/s, with ordinary stores 142; 832 tokens 3.7 us in a captured graph.
 struct RowsArgs {
   const uint8_t* pages;
   const int32_t* bt;
@@ -357,15 +333,25 @@ __global__ __launch_bounds__(kThreads) void cache_rows_fp4_kernel(const RowsArgs
     if (!rows) continue;
     const int g = w - (is_v ? a.hkv : 0);
     const uint8_t* const page = a.pages + (int64_t(in_pool ? blk : 0) * a.hkv + g) * kPage<D>;
-    uint32_t code[4], exp[4];
+    uint32_t code[4], exp[4];   // of the tokens 4 u + i (values), 4 i + u (keys)
+    if (is_v) {
+      const auto c = *reinterpret_cast<const typename Piece<D>::Lane*>(page + kValues<D> + lane * (D / 8));
+      const uint32_t e = *reinterpret_cast<const uint32_t*>(page + kValueScales<D> + grp * kBs + 4 * u);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {   // values: token 4 u + i; keys: 4 i + u
-      const int slot = is_v ? 4 * u + i : 4 * i + u;
-      const int at = is_v ? kValues<D> + lane * (D / 8) + i * (D / 32) : slot * (D / 2) + p * (D / 32);
-      code[i] = *reinterpret_cast<const Code*>(page + at);
-      exp[i] = page[is_v ? kValueScales<D> + grp * kBs + slot : kKeyScales<D> + slot * (D / 32) + grp];
-      if (!in_pool) code[i] = exp[i] = 0;
+      for (int i = 0; i < 4; ++i) {
+        code[i] = D == 128 ? c[i % (D / 32)] : c[i / 2] >> (16 * (i & 1));
+        exp[i] = e >> (8 * i) & 0xFFu;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        code[i] = *reinterpret_cast<const Code*>(page + (4 * i + u) * (D / 2) + p * (D / 32));
+        exp[i] = page[kKeyScales<D> + (4 * i + u) * (D / 32) + grp];
+      }
     }
+    if (!in_pool)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) code[i] = exp[i] = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = un.first + (is_v ? 4 * u + i : 4 * i + u);
@@ -378,7 +364,7 @@ __global__ __launch_bounds__(kThreads) void cache_rows_fp4_kernel(const RowsArgs
         o[3] = widen<3>(code[i], s);
       }
       if (t >= un.begin && t < un.end)
-        *reinterpret_cast<Words*>(rows + ((un.row0 + (t - un.P)) * a.hkv + g) * D + p * PC) = o;
+        __builtin_nontemporal_store(o, reinterpret_cast<Words*>(rows + ((un.row0 + (t - un.P)) * a.hkv + g) * D + p * PC));
     }
   }
 }
@@ -766,13 +752,20 @@ extern "C" cw_status cw_rope_append_fp4(const void* q, int64_t q_stride, const v
   a.num_blocks = num_blocks;
   a.rope_len = rope_len;
   a.pairs = rope ? rotary_dim / 2 : 0;
-  // Heads over grid y: a workgroup per CU at least, and two per unit, so that the last round of a
-  // large batch is short.
+  // Heads over grid y: a workgroup per CU at least; four per unit, eight where units hold many rows. us for 1, 2, 4,
+  // 8, 12 per unit: 1,030 units of about 15.7 rows, 48 heads of 128, 92, 88, 82, 79, 85; 160 units of 12.5, 36 heads,
+  // 15.2, 15.6, 12.4, 11.6, 11.4; 256 units of one row, 48 heads, 10.1, 8.3, 7.5, 9.7, 11.1.
   const int64_t heads = a.hq + 2 * int64_t(num_kv_heads), full = (heads + kWaves - 1) / kWaves;
-  const int64_t gy = std::min({full, int64_t(65535), std::max<int64_t>(2, (cw::kNumCu + units - 1) / units)});
-  auto* const kernel = head_dim == 128
-                           ? (interleaved ? rope_append_fp4_kernel<128, false> : rope_append_fp4_kernel<128, true>)
-                           : (interleaved ? rope_append_fp4_kernel<64, false> : rope_append_fp4_kernel<64, true>);
+  const int64_t gy = std::min({full, int64_t(65535), std::max<int64_t>(rows >= 8 * units ? 8 : 4, (cw::kNumCu + units - 1) / units)});
+  // More rows than the last-level cache (256 MiB) holds pass it: 16,128 rows of 48 heads of 128 (330 MB) 72 us against
+  // 79; 2,000 of 36 (32 MB) 12.0 against 11.6.
+  const bool once = rows * (2 * (a.hq + int64_t(num_kv_heads))) * head_dim * 2 > (int64_t(256) << 20);
+  auto pick = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    return interleaved ? (once ? rope_append_fp4_kernel<D, false, true> : rope_append_fp4_kernel<D, false, false>)
+                       : (once ? rope_append_fp4_kernel<D, true, true> : rope_append_fp4_kernel<D, true, false>);
+  };
+  auto* const kernel = head_dim == 128 ? pick(std::integral_constant<int, 128>()) : pick(std::integral_constant<int, 64>());
   hipLaunchKernelGGL(kernel, dim3(unsigned(units), unsigned(gy)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
   return check_launch("rope_append_fp4 launch");
 }

@@ -469,6 +469,7 @@ class BatchMeta:
         self.bt = self.cu = self.plen = self.plan = None
         self._split_plans = {}
         self._append_plans = {}
+        self._pointers = {}
         if device is not None:
             self.bt = torch.from_numpy(self.bt_host).to(device)
             self.cu = torch.from_numpy(self.cu_host).to(device)
@@ -510,7 +511,11 @@ class BatchMeta:
         return self._append_plans[num_blocks]
 
     def _hp(self, a):
-        return _ptr(a, ctypes.c_int32)
+        """The pointer object of one of this description's host arrays, made once."""
+        made = self._pointers.get(id(a))
+        if made is None or made[0] is not a:
+            made = self._pointers[id(a)] = (a, _ptr(a, ctypes.c_int32))
+        return made[1]
 
     def check_device_copies(self) -> None:
         """The caller guarantees that the device copies equal the host ones
@@ -775,6 +780,9 @@ def _rows(t: torch.Tensor, dtype, name: str, dev: int) -> tuple[int, int]:
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     shape, step = t.shape, t.stride()
+    if len(shape) == 3 and shape[0] > 1 and step[2] == 1 and step[1] == shape[2] and step[0] >= shape[1] * step[1] and \
+            t.dtype is dtype and t.get_device() == dev:   # (the usual case, of the checks below)
+        return t.data_ptr(), step[0]
     width = shape[-1]
     if step[-1] != 1 and width != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
