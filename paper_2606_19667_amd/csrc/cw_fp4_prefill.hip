@@ -29,6 +29,7 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kBlocks = kStep / kBs;
 static_assert(kWaves * 32 == cw::kTileRows, "one 32-column MFMA block per wave");
 static_assert(kWaves == 2 * kBlocks, "a wave stages one block of one tensor");
+constexpr int kMergeParts = 8;                // parts of a row that are merged in turn; more: side by side
 constexpr float kMaxSum = 0x1p30f;            // a row's base moves when its sum exceeds this
 
 // (Maxima that a NaN passes through: with NaN honoured fmaxf would quiet each operand first.)
@@ -178,9 +179,8 @@ void suffix_prefill_fp4_kernel(const PrefillArgs a) {
       ce += grid;
       e_next = fetch(ce);
     } else {
-      n_left = INT32_MAX;
+      e_left = INT32_MAX;
       n_keys = 0;
-      return;
     }
     n_left = min(e_left, 64);
     e_left -= n_left;
@@ -413,7 +413,7 @@ void suffix_prefill_fp4_kernel(const PrefillArgs a) {
       barrier();
     }
 
-    // ---- the entry's end (part of the next softmax interval): 64 columns at a time through the
+    // ---- the entry's end (part of the next softmax interval): 64 columns at a time (32 of a part) through the
     // wave's own area, so that whole lines are stored
     const float total = sum_pair32(l);
     if constexpr (SPLIT) {
@@ -421,15 +421,28 @@ void suffix_prefill_fp4_kernel(const PrefillArgs a) {
       // has to count in the merge, which takes a NaN log-sum-exp for an empty part: a large number stands there.)
       const bool any = __float_as_uint(total) != 0, bad = (__float_as_uint(total) & 0x7FFFFFFFu) > 0x7F800000u;
       const float inv = any ? 1.f / total : 0.f;
-      if (has_row(cur)) {
-        const int64_t at = int64_t(word(cur, cw::kEntSplit)) * a.part_rows + (int64_t(qrow0) + pos) * a.hq + g * a.group + hh;
+      const int64_t at0 = int64_t(word(cur, cw::kEntSplit)) * a.part_rows + int64_t(qrow0) * a.hq + g * a.group;
+      if (half == 0 && has_row(cur))
+        a.part_lse[at0 + int64_t(pos) * a.hq + hh] = bad ? 1e30f : any ? m + __builtin_amdgcn_logf(total) : -INFINITY;
+      uint8_t* const stg = lds + RING * G::STAGE + wave * G::OUT;
+      constexpr int OP = 32 * 4 + 16;
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+      for (int t = 0; t < DT; ++t) {
+        asm volatile("" ::: "memory");
 #pragma unroll
-          for (int gq = 0; gq < 4; ++gq)
-            *reinterpret_cast<f32x4*>(a.part_o + at * D + 32 * t + 8 * gq + 4 * half) =
-                f32x4{oacc[t][4 * gq] * inv, oacc[t][4 * gq + 1] * inv, oacc[t][4 * gq + 2] * inv, oacc[t][4 * gq + 3] * inv};
-        if (half == 0) a.part_lse[at] = bad ? 1e30f : any ? m + __builtin_amdgcn_logf(total) : -INFINITY;
+        for (int gq = 0; gq < 4; ++gq)
+          *reinterpret_cast<f32x4*>(stg + l32 * OP + gq * 32 + half * 16) =   // (0 times a masked NaN value is one)
+              any ? f32x4{oacc[t][4 * gq] * inv, oacc[t][4 * gq + 1] * inv, oacc[t][4 * gq + 2] * inv, oacc[t][4 * gq + 3] * inv}
+                  : f32x4{};
+        asm volatile("" ::: "memory");   // (as below: lanes read what other lanes of the wave wrote, in order)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int rr = i * 8 + lane / 8, mr = wave * 32 + rr;
+          const int hr = mr / a.per_tile, pr = mr - hr * a.per_tile;
+          const f32x4 x = *reinterpret_cast<const f32x4*>(stg + rr * OP + (lane & 7) * 16);
+          if (hr < a.group && pr < nvalid)
+            *reinterpret_cast<f32x4*>(a.part_o + (at0 + int64_t(pr) * a.hq + hr) * D + 32 * t + (lane & 7) * 4) = x;
+        }
       }
     } else {
       const float inv = has_row(cur) ? 1.f / total : 0.f;
@@ -529,7 +542,11 @@ cw_status prefill_fp4(const char* what, const void* q, const void* pages, const 
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return cw::fail(CW_EHIP, w + " launch: " + hipGetErrorString(e));
   if (!split) return cw::ok();
-  return cw_lse_merge(a.part_o, a.part_lse, splits, a.part_rows, head_dim, out, stream);
+  // The join takes a row's parts side by side, the merge in turn: 64 rows of 32 heads, 64 rows of 3 and of 4 times
+  // 32 heads (us of the call over 6,000 keys, captured, merge / join): 8 parts 33.6 / 33.4, 36.4 / 38.4, 39.7 / 42.2;
+  // 12 parts 32.1 / 30.6, 47.9 / 47.9, 49.6 / 50.0; 16 parts 32.4 / 29.7, 44.7 / 44.4, 50.3 / 49.2.
+  return splits > kMergeParts ? cw::decode_join(what, head_dim, a.part_o, a.part_lse, splits, a.part_rows, out, stream)
+                              : cw_lse_merge(a.part_o, a.part_lse, splits, a.part_rows, head_dim, out, stream);
 }
 
 }  // namespace

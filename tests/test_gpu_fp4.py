@@ -361,7 +361,7 @@ def _run_prefill(meta, q, cache, scale, splits):
                 cw.suffix_prefill_attn_split_fp4(meta, q, cache, scale, num_splits=splits))
 
 
-@pytest.mark.parametrize("splits", [0, 1, 3])
+@pytest.mark.parametrize("splits", [0, 1, 3, 12])
 @pytest.mark.parametrize("hq,hkv,D,key", [(8, 2, 128, 5), (8, 2, 128, 270), (14, 2, 64, 270), (2, 2, 64, 620), (2, 2, 64, 19)])
 def test_prefill_nan_scales(hq, hkv, D, key, splits):
     """A NaN scale of one KV head's key makes that head's rows that see it NaN, and nothing else; one of a value its
@@ -387,7 +387,7 @@ def test_prefill_nan_scales(hq, hkv, D, key, splits):
     assert np.array_equal(out[keep], clean[keep])
 
 
-@pytest.mark.parametrize("splits", [0, 3])
+@pytest.mark.parametrize("splits", [0, 3, 11])
 @pytest.mark.parametrize("D", [64, 128])
 def test_prefill_scores_that_grow_by_orders(D, splits):
     """Keys whose scales grow along the prompt: the softmax base moves, several times in a row's steps; and shrink:
@@ -412,7 +412,7 @@ def test_prefill_scores_that_grow_by_orders(D, splits):
         _within(out, exp, (2 * B8 + 2.0 ** -12 + 2 * score * 2.0 ** -22) * mag + B8 * np.abs(exp) + lost, name)
 
 
-@pytest.mark.parametrize("splits", [0, 3])
+@pytest.mark.parametrize("splits", [0, 3, 11])
 @pytest.mark.parametrize("D", [64, 128])
 def test_prefill_ends_beside_values_out_of_range(D, splits):
     """One head's values are near 2^126, so its rows' sums may leave fp32; one of its query rows is NaN. The call
@@ -458,7 +458,7 @@ SPLIT_CASES = [
 
 
 @pytest.mark.parametrize("hq,hkv,D,P,S", SPLIT_CASES)
-@pytest.mark.parametrize("splits", [None, 1, 2, 7, 64])
+@pytest.mark.parametrize("splits", [None, 1, 2, 7, 9, 64])
 def test_prefill_split(hq, hkv, D, P, S, splits):
     """Runs of keys, some of them empty (short prompts) or unseen by some rows, joined."""
     _say(f"split prefill {hq}/{hkv} D={D} P={P} S={S} x{splits}")
