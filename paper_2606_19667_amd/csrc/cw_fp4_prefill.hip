@@ -29,7 +29,8 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kBlocks = kStep / kBs;
 static_assert(kWaves * 32 == cw::kTileRows, "one 32-column MFMA block per wave");
 static_assert(kWaves == 2 * kBlocks, "a wave stages one block of one tensor");
-constexpr int kMergeParts = 8;                // parts of a row that are merged in turn; more: side by side
+constexpr int kMergeParts = 8;                // parts of a row that are merged in turn; more: side by side, for
+constexpr int64_t kJoinRows = 16384;          // this many rows at most (a workgroup each)
 constexpr float kMaxSum = 0x1p30f;            // a row's base moves when its sum exceeds this
 
 // (Maxima that a NaN passes through: with NaN honoured fmaxf would quiet each operand first.)
@@ -544,9 +545,11 @@ cw_status prefill_fp4(const char* what, const void* q, const void* pages, const 
   if (!split) return cw::ok();
   // The join takes a row's parts side by side, the merge in turn: 64 rows of 32 heads, 64 rows of 3 and of 4 times
   // 32 heads (us of the call over 6,000 keys, captured, merge / join): 8 parts 33.6 / 33.4, 36.4 / 38.4, 39.7 / 42.2;
-  // 12 parts 32.1 / 30.6, 47.9 / 47.9, 49.6 / 50.0; 16 parts 32.4 / 29.7, 44.7 / 44.4, 50.3 / 49.2.
-  return splits > kMergeParts ? cw::decode_join(what, head_dim, a.part_o, a.part_lse, splits, a.part_rows, out, stream)
-                              : cw_lse_merge(a.part_o, a.part_lse, splits, a.part_rows, head_dim, out, stream);
+  // 12 parts 32.1 / 30.6, 47.9 / 47.9, 49.6 / 50.0; 16 parts 32.4 / 29.7, 44.7 / 44.4, 50.3 / 49.2. 8 times 64 rows,
+  // 2,000 keys: 12 parts 55.5 / 57.2, 16 parts 67.5 / 65.6.
+  const bool join = splits > kMergeParts && a.part_rows <= kJoinRows;
+  return join ? cw::decode_join(what, head_dim, a.part_o, a.part_lse, splits, a.part_rows, out, stream)
+              : cw_lse_merge(a.part_o, a.part_lse, splits, a.part_rows, head_dim, out, stream);
 }
 
 }  // namespace

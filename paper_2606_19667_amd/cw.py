@@ -511,10 +511,14 @@ class BatchMeta:
         return self._append_plans[num_blocks]
 
     def _hp(self, a):
-        """The pointer object of one of this description's host arrays, made once."""
-        made = self._pointers.get(id(a))
+        return _ptr(a, ctypes.c_int32)
+
+    def _field(self, name: str):
+        """The pointer object of the host array of that name, made anew when the field is."""
+        a = getattr(self, name)
+        made = self._pointers.get(name)
         if made is None or made[0] is not a:
-            made = self._pointers[id(a)] = (a, _ptr(a, ctypes.c_int32))
+            made = self._pointers[name] = (a, self._hp(a))
         return made[1]
 
     def check_device_copies(self) -> None:
@@ -1158,7 +1162,7 @@ def rope_append_fp4(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp
         0 if rope is None else rope.shape[0], 0 if rope is None else 2 * rope.shape[1], 1 if interleaved else 0,
         None if q_out is None else _arg(q_out, bf16, "q_out", dev), cache._arg(hkv, D, dev),
         _arg(meta.bt, i32, "block_table", dev), meta.bt_stride, _arg(meta.cu, i32, "cu_suffix", dev),
-        _arg(meta.plen, i32, "prefix_len", dev), meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv,
+        _arg(meta.plen, i32, "prefix_len", dev), meta._field("cu_host"), meta._field("plen_host"), meta.batch, hq, hkv,
         D, BLOCK_SIZE, cache.num_blocks, _stream_of(stream, dev)))
     return q_out
 
@@ -1182,8 +1186,8 @@ def cache_rows_fp4(meta: BatchMeta, cache: Fp4KvCache, k_rows: torch.Tensor | No
             raise ValueError(f"{name} must be {list(shape)}, got {tuple(t.shape)}")
     _check(_lib.cw_cache_rows_fp4(
         cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
-        _arg(meta.cu, i32, "cu_suffix", dev), _arg(meta.plen, i32, "prefix_len", dev), meta._hp(meta.cu_host),
-        meta._hp(meta.plen_host), meta.batch, hkv, D, BLOCK_SIZE, cache.num_blocks, _arg(k_rows, bf16, "k_rows", dev),
+        _arg(meta.cu, i32, "cu_suffix", dev), _arg(meta.plen, i32, "prefix_len", dev), meta._field("cu_host"),
+        meta._field("plen_host"), meta.batch, hkv, D, BLOCK_SIZE, cache.num_blocks, _arg(k_rows, bf16, "k_rows", dev),
         _arg(v_rows, bf16, "v_rows", dev), _stream_of(stream, dev)))
     return k_rows, v_rows
 
@@ -1207,8 +1211,8 @@ def suffix_prefill_attn_fp4(meta: BatchMeta, q: torch.Tensor, cache: Fp4KvCache,
     dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
     _check(_lib.cw_suffix_prefill_attn_fp4(
         _arg(q, bf16, "q", dev), cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
-        meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.num_blocks,
-        softmax_scale, meta._hp(meta.plan_host), _arg(meta.plan, i32, "plan", dev), _arg(out, bf16, "out", dev),
+        meta._field("cu_host"), meta._field("plen_host"), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.num_blocks,
+        softmax_scale, meta._field("plan_host"), _arg(meta.plan, i32, "plan", dev), _arg(out, bf16, "out", dev),
         _stream_of(stream, dev)))
     return out
 
@@ -1251,7 +1255,7 @@ def suffix_prefill_attn_split_fp4(meta: BatchMeta, q: torch.Tensor, cache: Fp4Kv
     dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
     _check(_lib.cw_suffix_prefill_attn_split_fp4(
         _arg(q, bf16, "q", dev), cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
-        meta._hp(meta.cu_host), meta._hp(meta.plen_host), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.num_blocks,
+        meta._field("cu_host"), meta._field("plen_host"), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.num_blocks,
         softmax_scale, meta._hp(plan_host), _arg(plan_dev, i32, "plan", dev),
         _arg(workspace, torch.uint8, "workspace", dev), workspace.numel(), _arg(out, bf16, "out", dev),
         _stream_of(stream, dev)))

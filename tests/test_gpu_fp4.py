@@ -454,6 +454,7 @@ SPLIT_CASES = [
     (28, 4, 128, [700, 40], [40, 3]),
     (4, 1, 64, [5000, 3, 4100], [9, 70, 64]),
     (128, 2, 64, [130], [5]),
+    (64, 4, 64, [700, 50], [260, 41]),
 ]
 
 
