@@ -90,7 +90,7 @@ struct Geom {
 // The two waves of a SIMD alternate. A step j of a wave takes two intervals, each ended by a
 // workgroup barrier:
 //   softmax(j):   2^x packed to bf16, row sums (vector work)
-//   products(j):  O^T += V(j)^T P(j)^T, then S(j + 1) = K(j + 1) Q^T (matrix work); beside the latter's
+//   products(j):  O^T += V(j)^T P(j)^T, then S(j + 1) = K(j + 1) Q^T (matrix work); beside the last
 //                 products four codes each of step j + 2 are converted and written to LDS, then the loads
 //                 of step j + 3 go out
 // Waves 4-7 (group 1) run one interval behind waves 0-3. After an entry's last step S(j + 1) is the
@@ -308,10 +308,13 @@ void suffix_prefill_fp4_kernel(const PrefillArgs a) {
   for (int t = 0; t < DT; ++t) oacc[t] = f32x16{};
   const bf16x2 ones{(__bf16)1.0f, (__bf16)1.0f};
 
-  constexpr int RA = 6;   // operands in flight ahead of their MFMA
+  constexpr int RA = 4;   // operands in flight ahead of their MFMA
   constexpr int NPV = kBlocks * DT, NQK = 2 * KS, N = NPV + NQK;
-  constexpr int LOAD_AT = N - 5;   // the product that the next loads go out beside
-  static_assert(NPV + G::UNITS - 1 <= LOAD_AT, "the loaded codes are converted before they are replaced");
+  // The loaded codes are converted beside the last products and the next loads go out beside the last of these: the
+  // later, the more time a load has. us with both from the first QK product on, 6 operands ahead / so: 8 x 2,112 rows
+  // behind 3,136 keys 988 / 976, 6 x ~411 behind ~700 47.6 / 46.5, 1 x 2,000 54.8 / 53.5; twice the conversions beside
+  // each of half as many products 980, 46.9, 53.5; a further step of loads in flight, copied into place 991, 47.4, 54.9.
+  constexpr int WIDEN_AT = N - G::UNITS;
   bf16x8 op[RA];
   int st0 = 0, st1 = G::STAGE, st2 = 2 * G::STAGE;   // LDS places of the current step and the two after it
   auto row_max = [&]() __attribute__((always_inline)) -> float {   // of the current step's scaled scores
@@ -398,11 +401,11 @@ void suffix_prefill_fp4_kernel(const PrefillArgs a) {
           sc[q & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % RA], qf[q >> 1], q < 2 ? f32x16{} : sc[q & 1], 0, 0, 0);
         }
         if (i + RA < N) op[i % RA] = i + RA < NPV ? rdv(vb, i + RA) : rdk(kb, i + RA - NPV);
-        if (i >= NPV && i < NPV + G::UNITS) {
-          widen4(i - NPV);
-          stage(st2, i - NPV);
+        if (i >= WIDEN_AT) {
+          widen4(i - WIDEN_AT);
+          stage(st2, i - WIDEN_AT);
         }
-        if (i == LOAD_AT) load();
+        if (i == N - 1) load();
         __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_s_setprio(0);
