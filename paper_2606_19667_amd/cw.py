@@ -1122,11 +1122,13 @@ class Fp4KvCache:
     def head_dim(self) -> int:
         return int(self.pages.shape[2]) // 17
 
-    def _arg(self, num_kv_heads: int, head_dim: int, dev: int) -> int:
-        if self.pages.shape[1:] != (num_kv_heads, 17 * head_dim):
+    def _args(self, num_kv_heads: int, head_dim: int, dev: int) -> tuple[int, int]:
+        """(address, number of blocks) for a call with such heads on GPU `dev`."""
+        blocks, heads, width = self.pages.shape
+        if heads != num_kv_heads or width != 17 * head_dim:
             raise ValueError(f"the cache holds {self.num_kv_heads} KV heads of {self.head_dim}, "
                              f"the call has {num_kv_heads} of {head_dim}")
-        return _arg(self.pages, torch.uint8, "cache.pages", dev)
+        return _arg(self.pages, torch.uint8, "cache.pages", dev), blocks
 
 
 def rope_append_fp4(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp4KvCache,
@@ -1142,11 +1144,14 @@ def rope_append_fp4(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp
     if DEBUG_CHECK_COPIES:
         meta.check_device_copies()
     hq, hkv, D, T = meta.num_q_heads, meta.num_kv_heads, meta.head_dim, int(meta.cu_host[-1])
-    for name, t, h in (("q", q, hq), ("k", k, hkv), ("v", v, hkv)):
-        if t is not None and t.shape != (T, h, D):
-            raise ValueError(f"{name} must be [{T}, {h}, {D}], got {tuple(t.shape)}")
-    if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2):
-        raise ValueError(f"rope must be [n, pairs, 2], got {tuple(rope.shape)}")
+    for name, t, shape in (("q", q, (T, hq, D)), ("k", k, (T, hkv, D)), ("v", v, (T, hkv, D))):
+        if t is not None and t.shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}, got {tuple(t.shape)}")
+    rope_len, pairs = 0, 0
+    if rope is not None:
+        if rope.dim() != 3 or rope.shape[2] != 2:
+            raise ValueError(f"rope must be [n, pairs, 2], got {tuple(rope.shape)}")
+        rope_len, pairs = rope.shape[:2]
     if q is None and q_out is not None:
         raise ValueError("q_out without q")
     if q is not None and q_out is None:
@@ -1157,13 +1162,14 @@ def rope_append_fp4(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp
     pk, sk = _rows(k, bf16, "k", dev)
     pv, sv = _rows(v, bf16, "v", dev)
     pq, sq = (None, 0) if q is None else _rows(q, bf16, "q", dev)
+    pages, num_blocks = cache._args(hkv, D, dev)
     _check(_lib.cw_rope_append_fp4(
         pq, sq, pk, sk, pv, sv, None if rope is None else _arg(rope, torch.float32, "rope", dev),
-        0 if rope is None else rope.shape[0], 0 if rope is None else 2 * rope.shape[1], 1 if interleaved else 0,
-        None if q_out is None else _arg(q_out, bf16, "q_out", dev), cache._arg(hkv, D, dev),
+        rope_len, 2 * pairs, 1 if interleaved else 0,
+        None if q_out is None else _arg(q_out, bf16, "q_out", dev), pages,
         _arg(meta.bt, i32, "block_table", dev), meta.bt_stride, _arg(meta.cu, i32, "cu_suffix", dev),
         _arg(meta.plen, i32, "prefix_len", dev), meta._field("cu_host"), meta._field("plen_host"), meta.batch, hq, hkv,
-        D, BLOCK_SIZE, cache.num_blocks, _stream_of(stream, dev)))
+        D, BLOCK_SIZE, num_blocks, _stream_of(stream, dev)))
     return q_out
 
 
@@ -1184,10 +1190,11 @@ def cache_rows_fp4(meta: BatchMeta, cache: Fp4KvCache, k_rows: torch.Tensor | No
     for name, t in (("k_rows", k_rows), ("v_rows", v_rows)):
         if t.shape != shape:
             raise ValueError(f"{name} must be {list(shape)}, got {tuple(t.shape)}")
+    pages, num_blocks = cache._args(hkv, D, dev)
     _check(_lib.cw_cache_rows_fp4(
-        cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
+        pages, _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
         _arg(meta.cu, i32, "cu_suffix", dev), _arg(meta.plen, i32, "prefix_len", dev), meta._field("cu_host"),
-        meta._field("plen_host"), meta.batch, hkv, D, BLOCK_SIZE, cache.num_blocks, _arg(k_rows, bf16, "k_rows", dev),
+        meta._field("plen_host"), meta.batch, hkv, D, BLOCK_SIZE, num_blocks, _arg(k_rows, bf16, "k_rows", dev),
         _arg(v_rows, bf16, "v_rows", dev), _stream_of(stream, dev)))
     return k_rows, v_rows
 
@@ -1209,9 +1216,10 @@ def suffix_prefill_attn_fp4(meta: BatchMeta, q: torch.Tensor, cache: Fp4KvCache,
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
     dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
+    pages, num_blocks = cache._args(hkv, D, dev)
     _check(_lib.cw_suffix_prefill_attn_fp4(
-        _arg(q, bf16, "q", dev), cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
-        meta._field("cu_host"), meta._field("plen_host"), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.num_blocks,
+        _arg(q, bf16, "q", dev), pages, _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
+        meta._field("cu_host"), meta._field("plen_host"), meta.batch, hq, hkv, D, BLOCK_SIZE, num_blocks,
         softmax_scale, meta._field("plan_host"), _arg(meta.plan, i32, "plan", dev), _arg(out, bf16, "out", dev),
         _stream_of(stream, dev)))
     return out
@@ -1253,9 +1261,10 @@ def suffix_prefill_attn_split_fp4(meta: BatchMeta, q: torch.Tensor, cache: Fp4Kv
         workspace = _new(stream, max(need, 1), torch.uint8, q.device)
     plan_host, plan_dev = meta.split_plan(int(num_splits))
     dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
+    pages, num_blocks = cache._args(hkv, D, dev)
     _check(_lib.cw_suffix_prefill_attn_split_fp4(
-        _arg(q, bf16, "q", dev), cache._arg(hkv, D, dev), _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
-        meta._field("cu_host"), meta._field("plen_host"), meta.batch, hq, hkv, D, BLOCK_SIZE, cache.num_blocks,
+        _arg(q, bf16, "q", dev), pages, _arg(meta.bt, i32, "block_table", dev), meta.bt_stride,
+        meta._field("cu_host"), meta._field("plen_host"), meta.batch, hq, hkv, D, BLOCK_SIZE, num_blocks,
         softmax_scale, meta._hp(plan_host), _arg(plan_dev, i32, "plan", dev),
         _arg(workspace, torch.uint8, "workspace", dev), workspace.numel(), _arg(out, bf16, "out", dev),
         _stream_of(stream, dev)))
@@ -1313,9 +1322,10 @@ def decode_attn_fp4(q: torch.Tensor, cache: Fp4KvCache, block_table: torch.Tenso
     if workspace is None and need:
         workspace = _new(stream, need, torch.uint8, q.device)
     dev, bf16, i32 = _device(q, "q"), torch.bfloat16, torch.int32
+    pages, num_blocks = cache._args(hkv, D, dev)
     _check(_lib.cw_decode_attn_fp4(
-        _arg(q, bf16, "q", dev), cache._arg(hkv, D, dev), _arg(block_table, i32, "block_table", dev), stride,
-        _arg(seq_lens, i32, "seq_lens", dev), B, hq, hkv, D, BLOCK_SIZE, cache.num_blocks, softmax_scale, num_splits,
+        _arg(q, bf16, "q", dev), pages, _arg(block_table, i32, "block_table", dev), stride,
+        _arg(seq_lens, i32, "seq_lens", dev), B, hq, hkv, D, BLOCK_SIZE, num_blocks, softmax_scale, num_splits,
         None if workspace is None else _arg(workspace, torch.uint8, "workspace", dev),
         0 if workspace is None else workspace.numel(), _arg(out, bf16, "out", dev), _stream_of(stream, dev)))
     return out
