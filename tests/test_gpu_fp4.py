@@ -765,6 +765,41 @@ def test_blocks_beyond_32_bit_offsets():
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_appends_of_more_rows_than_caches_hold_equal_their_parts(D, interleaved):
+    """8,200 rows of 8,192 query columns (273 MB or more with what is written) in a call have the bits of a call for each request."""
+    hq, hkv, P, S = 8192 // D, 2, [3, 16], [4100, 4100]
+    stride = (16 + 4100 + 15) // 16
+    bt = np.arange(2 * stride, dtype=np.int32).reshape(2, stride)[:, ::-1].copy()
+    g = torch.Generator(device="cuda").manual_seed(95)
+    qkv = torch.randn(8200, (hq + 2 * hkv) * D, generator=g, device="cuda").to(torch.bfloat16)
+    q, k, v = (x.view(8200, -1, D) for x in qkv.split([hq * D, hkv * D, hkv * D], 1))
+    rope = _table(4200, D)
+    caches = [cw.Fp4KvCache.of(torch.zeros(2 * stride, hkv, 17 * D, dtype=torch.uint8, device="cuda")) for _ in range(2)]
+    whole = cw.rope_append_fp4(cw.BatchMeta(bt, [0, 4100, 8200], P, hq, hkv, D), k, v, caches[0], q=q, rope=rope,
+                               interleaved=interleaved)
+    for r in range(2):
+        rows = slice(4100 * r, 4100 * (r + 1))
+        part = cw.rope_append_fp4(cw.BatchMeta(bt[r:r + 1], [0, 4100], P[r:r + 1], hq, hkv, D), k[rows], v[rows],
+                                  caches[1], q=q[rows], rope=rope, interleaved=interleaved)
+        assert torch.equal(_bits(part), _bits(whole[rows]))
+    assert torch.equal(caches[0].pages, caches[1].pages)
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_with_a_table_of_more_than_caches_hold(D, splits):
+    """A table that could name 272 MB of pages or more: the bits that the table of the sequences' own blocks gives."""
+    b = Batch(12, 4, D, [700, 33, 5], [0, 0, 0], seed=96)
+    wide = np.full((3, 21000), -1, np.int32)
+    wide[:, :b.bt.shape[1]] = b.bt
+    q, lens = b.queries(3).cuda(), torch.tensor([700, 33, 0], dtype=torch.int32).cuda()
+    got, want = (cw.decode_attn_fp4(q, b.cache, torch.from_numpy(np.ascontiguousarray(x)).cuda(), lens, D ** -0.5,
+                                    num_splits=splits) for x in (wide, b.bt))
+    assert torch.equal(_bits(got), _bits(want)) and not want[2].any() and not want.isnan().any()
+
+
 def test_decode_calls_at_once_on_two_streams():
     """Two calls at the same time with workspaces that they allocate themselves."""
     b = Batch(8, 2, 128, [900, 300], [0, 0], seed=54)
