@@ -721,7 +721,7 @@ cw_status cw_decode_attn_fp8(const void* q, const void* k8, const void* v8, cons
  * (2 j, 2 j + 1), j < n:
  *   rot(u)[a] = u[a] cos_pj - u[b] sin_pj,  rot(u)[b] = u[b] cos_pj + u[a] sin_pj
  * and the columns from rotary_dim on stay as they are.
- *   q_out[t][h] = bf16(rot(q[t][h])), rotated in fp32
+ *   q_out[t][h] = bf16(rot(q[t][h])), rotated in fp32 (what leaves it is infinite)
  *   K rows rot(k[t][g]), V rows v[t][g], 32 columns at a time, with amax their
  *     largest magnitude:
  *     scale = 2^e, e the smallest in [-100, 125] with amax <= 7 * 2^e

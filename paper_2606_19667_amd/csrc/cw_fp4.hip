@@ -248,8 +248,10 @@ __global__ __launch_bounds__(kThreads) void rope_append_fp4_kernel(const AppendA
           x[2 * j + 1] = turns ? y1 : hi;
         }
       };
-      turn_all(turned);
-      if (!is_q) {
+      if (is_q) {   // (an infinite value stays one: turned would subtract it from itself)
+        turn_all([](float x, float w, float c, float s) __attribute__((always_inline)) { return fmaf(x, c, -(w * s)); });
+      } else {
+        turn_all(turned);
         bool near = false;
 #pragma unroll
         for (int j = 0; j < PC; ++j) near |= ((__float_as_uint(x[j]) + 4) & 0x1FFFFFu) <= 8 && x[j] != 0.f;

@@ -5,7 +5,7 @@ Bounds, derived from the roundings (eps/2 of bf16 is 2^-8):
 
 * append: pages are compared byte by byte with the oracle's, which rounds the rotation in 64 bits:
   the call's codes are those of exact arithmetic. q is an output rounding, 2^-8 |q|, plus the
-  rotation's: at most 1.5 units of 2^-23 of the result, taken as 2^-22 of the products' magnitudes.
+  rotation's: 2^-24 of a product and of the sum, taken as 2^-22 of the products' magnitudes.
 * rows: exact.
 * attention: with A = sum p|v| / sum p, the probabilities' rounding to bf16 before the product
   gives 2^-8 A; the row's sum of the same rounded values 2^-8 |o| <= 2^-8 A; fp32 scores of
@@ -210,6 +210,30 @@ def test_append_values_of_any_size(D, rotate):
     torch.cuda.synchronize()
     with np.errstate(invalid="ignore"):
         _check_append(b, None, k, v, rope, False, None, "any size")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("part,interleaved", [(1, False), (0.5, False), (1, True)])
+def test_append_queries_of_any_size(D, part, interleaved):
+    """Queries from bf16's smallest to near its largest values, infinities and NaN: what the formula gives of them."""
+    b = Batch(4, 2, D, [5], [70], seed=64, held=[5])
+    q, k, v = _append_inputs(b)
+    size = torch.exp2(torch.randint(-133, 120, (70, 4, D // 32), generator=b.g).float()).repeat_interleave(32, 2)
+    x = q.float().cpu() * size
+    x[5, 0, 7], x[6, 1, 33], x[7, 0, D - 1], x[8, 3, 0] = float("nan"), float("inf"), -float("inf"), float("inf")
+    q.copy_(x.to(torch.bfloat16))
+    rope = _table(80, int(part * D))
+    got = _f64(cw.rope_append_fp4(b.meta(), k, v, b.cache, q=q, rope=rope, interleaved=interleaved))
+    cos_sin = _f64(rope)[b.positions()]
+    with np.errstate(invalid="ignore"):
+        exp = F.rotate(_f64(q), cos_sin, interleaved)
+        # |x c| + |w s|: the rotation of magnitudes by (|c|, -|s|) has it in a pair's first column, by (|c|, |s|) in its second
+        mag = [F.rotate(np.abs(_f64(q)), np.stack([np.abs(cos_sin[..., 0]), s * np.abs(cos_sin[..., 1])], -1), interleaved)
+               for s in (-1, 1)]
+    whole = np.isfinite(exp)
+    assert (~whole).sum() >= 4 and np.array_equal(got[~whole], exp[~whole], equal_nan=True)
+    # output's rounding, of its smallest steps too; product and sum, half a unit of 2^-23 each
+    _within(got[whole], exp[whole], B8 * np.abs(exp[whole]) + 2.0 ** -23 * np.maximum(*mag)[whole] + 2.0 ** -133, f"D={D}")
 
 
 def test_append_drops_blocks_outside_the_pool_and_long_tables():
