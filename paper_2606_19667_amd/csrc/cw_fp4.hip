@@ -819,8 +819,9 @@ extern "C" int64_t cw_decode_attn_fp4_workspace_bytes(int32_t batch, int32_t num
   if (batch < 1 || num_q_heads < 1 || (head_dim != 64 && head_dim != 128) || num_splits < 1 ||
       num_splits > cw::kMaxSplits)
     return cw::fail(CW_EINVAL, "decode_attn_fp4_workspace_bytes: invalid argument");
-  if (num_splits == 1) return 0;
   const int64_t rows = int64_t(batch) * num_q_heads;
+  if (rows > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, "decode_attn_fp4_workspace_bytes: batch too large");
+  if (num_splits == 1) return 0;
   return lse_offset(rows, head_dim, num_splits) + int64_t(num_splits) * rows * 4;
 }
 
@@ -846,6 +847,7 @@ extern "C" cw_status cw_decode_attn_fp4(const void* q, const void* pages, const 
   if (num_splits < 1 || num_splits > cw::kMaxSplits) return cw::fail(CW_EINVAL, w + ": num_splits must be in [1, 64]");
   if (!aligned16(q) || !aligned16(out)) return cw::fail(CW_EINVAL, w + ": pointers must be 16-byte aligned");
   const int64_t need = cw_decode_attn_fp4_workspace_bytes(batch, num_q_heads, head_dim, num_splits);
+  if (need < 0) return cw_status(need);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return cw::fail(CW_EINVAL, w + ": workspace must hold " + std::to_string(need) + " bytes, 16-byte aligned");
   DecodeArgs a;
@@ -872,7 +874,7 @@ extern "C" cw_status cw_decode_attn_fp4(const void* q, const void* pages, const 
   a.by_heads = FastDiv(num_kv_heads);
   a.c_log2 = softmax_scale * 1.4426950408889634f;
   const int64_t grid = int64_t(batch) * num_kv_heads * head_tiles * num_splits;
-  if (grid > kMaxGrid || rows > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
+  if (grid > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
   auto* const s = static_cast<hipStream_t>(stream);
   // A cache that the last-level cache (256 MiB) cannot hold is read past it. us, 64 requests of about 10,367 tokens,
   // 720 MB: 138 against 153; 8 heads of 9,000 tokens, 10 MB, read again and again: 60 against 55.

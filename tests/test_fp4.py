@@ -237,7 +237,7 @@ def _decode(q=d_, pages=d_, bt=d_, stride=4, lens=d_, batch=2, hq=8, hkv=2, d=64
     (E, dict(splits=2, ws=d_, wb=2 * 16 * 65 * 4 - 1)), (E, dict(splits=2, ws=odd, wb=1 << 20)), (E, dict(q=odd)),
     (E, dict(out=odd)), (E, dict(pages=odd)), (U, dict(d=32)), (U, dict(bs=32)), (U, dict(hq=2 * 129)),
     (U, dict(stride=2 ** 27)), (U, dict(stride=2 ** 27 - 256)), (U, dict(batch=2 ** 30, splits=1)),
-    (U, dict(batch=2 ** 23, splits=1)),
+    (U, dict(batch=2 ** 23, splits=1)), (U, dict(batch=2 ** 30, hkv=2 ** 16, hq=2 ** 23, splits=64, ws=d_, wb=2 ** 40)),
 ])
 def test_decode_refusals(status, change):
     assert _decode(**change) == status
@@ -251,6 +251,8 @@ def test_decode_workspace_and_split_counts():
     for bad in ((0, 32, 128, 1), (4, 0, 128, 1), (4, 32, 96, 1), (4, 32, 128, 0), (4, 32, 128, 65)):
         with pytest.raises(cw.CwError):
             f(*bad)
+    with pytest.raises(cw.CwError, match="too large"):   # (its bytes would pass 64 bits)
+        f(2 ** 31 - 1, 2 ** 31 - 1, 128, 64)
     for b, hq, hkv, n in ((1, 32, 8, 1), (1, 32, 8, 200), (16, 32, 8, 1408), (64, 64, 8, 10368), (1, 4, 1, 10 ** 6)):
         assert 1 <= cw.decode_split_count_fp4(b, hq, hkv, n) <= 64
     assert cw.decode_split_count_fp4(1, 32, 8, 1) == 1
