@@ -102,7 +102,7 @@ struct Geom {
 // replaces (step x - 3) was last read in 2 x - 4.
 //
 // 8 requests of 2,112 rows behind 3,136 keys, 32 / 8 heads of 128: 960 to 1,005 us by card, 1.2 PFLOP/s, what a large library
-// product of bf16 reaches on the same card (1.18): the matrix pipe is busy 57 % of the cycles at 2.04 GHz, and a fourth
+// product of bf16 reaches on the same card (1.18): the matrix pipe is busy 58 % of the cycles at 2.0 GHz, and a fourth
 // less matrix work takes 13 % off, 32 multiply-adds less of the softmax nothing. A step of lightly loaded units is 1.2 to
 // 1.4 us. 6 x ~411 rows behind ~700 keys, 28 / 4 heads, 42 us: the longest entry's 24 steps, behind a start in which
 // every workgroup reads its queries and three steps' pages (29 MB).
