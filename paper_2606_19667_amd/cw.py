@@ -521,6 +521,10 @@ class BatchMeta:
             made = self._pointers[name] = (a, self._hp(a))
         return made[1]
 
+    def __getstate__(self):
+        # (for copies and pickles: a pointer object's own holds the array's first number, not the array)
+        return {**self.__dict__, "_pointers": {}}
+
     def check_device_copies(self) -> None:
         """The caller guarantees that the device copies equal the host ones
         (the library validates and plans with the host copies, the kernels

@@ -1,5 +1,7 @@
 """The 4-bit cache without a GPU: pins of its oracle, and the refusals of the calls."""
+import copy
 import ctypes
+import pickle
 
 import numpy as np
 import pytest
@@ -307,3 +309,25 @@ def test_4_bit_sources_are_built_with_nan_honoured():
     for s in sources:
         honor = [f for f in build.HIP_FLAGS + build.EXTRA_FLAGS.get(s, []) if f.endswith("honor-nans")]
         assert honor[-1] == "-fhonor-nans", s
+
+
+@pytest.mark.parametrize("again", [copy.copy, copy.deepcopy, lambda m: pickle.loads(pickle.dumps(m))], ids=["copy", "deepcopy", "pickle"])
+def test_copies_of_a_used_batch_hand_over_their_own_arrays(again):
+    """What a call keeps of a batch's host arrays goes into the library as their address: a copy of the batch, or one
+    that another process gets, has to hand over the whole of its own."""
+    def address(p):   # (arrays that cannot be written have a pointer, others an object on their memory)
+        return ctypes.addressof(p.contents if isinstance(p, ctypes.POINTER(ctypes.c_int32)) else p)
+
+    for writable in (True, False):
+        meta = cw.BatchMeta(np.zeros((3, 4)), [0, 2, 5, 9], [5, 0, 7], 8, 2, 64, device=None)
+        names = ("cu_host", "plen_host", "plan_host")
+        for name in names:
+            getattr(meta, name).flags.writeable = writable
+            meta._field(name)
+        other = again(meta)
+        for m in (meta, other):
+            for name in names:
+                assert address(m._field(name)) == getattr(m, name).ctypes.data, (name, writable)
+        other.cu_host = np.array([0, 1, 2, 3], np.int32)   # (and the other one does not follow)
+        assert address(other._field("cu_host")) == other.cu_host.ctypes.data
+        assert address(meta._field("cu_host")) == meta.cu_host.ctypes.data
