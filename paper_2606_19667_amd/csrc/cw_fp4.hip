@@ -388,8 +388,9 @@ __global__ __launch_bounds__(kThreads) void cache_rows_fp4_kernel(const RowsArgs
 //    D / 16 c + j. A conversion gives two columns of a token, and a byte permute two tokens of a
 //    column.
 // The base of a column's exponents is the row maximum of the wave's first chunk and moves only when
-// a sum passes 2^30 (bf16 and fp32 have the range), so later chunks need no maximum. The row's sum
-// takes the probabilities as they are rounded for the product.
+// a lane's sum passes 2^26 (bf16 and fp32 have the range), so later chunks need no maximum. Four lanes hold parts of
+// a column's sum and four waves join unnormalised: weights of 2^30 in all, so values up to 2^96 stay in fp32's range.
+// The row's sum takes the probabilities as they are rounded for the product.
 // HBM-bound when sequences are long: 64 requests of about 10,367 tokens, 64 / 8 heads of 128 (720 MB) 136 us, 5.3 TB/s
 // (a copy 4.8 to 5.3). Of few chunks it is bound by the chain of length, table word, codes, scores, softmax, product
 // and join (4.2 us for 300 tokens of 4 heads of 64), and by a wave's instructions: a chunk is 146 vector ones, 64 of
@@ -423,7 +424,7 @@ struct DecodeArgs {
 
 constexpr int kChunk = 32;      // keys of a wave's step: two blocks
 constexpr int kTileHeads = 16;
-constexpr float kMaxSum = 0x1p30f;
+constexpr float kMaxSum = 0x1p26f;   // of a lane's part of a column's sum
 
 constexpr int kAhead = 1;       // chunks in flight ahead of the one that a wave works on
 constexpr int kRawBuffer = 0x00027000;   // a buffer's last word: bytes at offsets, checked against its size

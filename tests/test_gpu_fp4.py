@@ -569,6 +569,56 @@ def test_decode_scores_that_grow_by_orders(D, splits):
         _within(_f64(out), exp, (2 * B8 + 2.0 ** -12 + 2 * score * 2.0 ** -22) * mag + B8 * np.abs(exp) + lost, name)
 
 
+def _large_values(D, pattern, step, times, power=96):
+    """A batch of one request whose values reach 2^power and whose scores (base 2, queries of ones, a softmax scale of
+    ln 2) are pattern[i % len] in the i-th `step` keys, the pattern `times` times (but for the last 5 keys)."""
+    n = step * times * len(pattern) - 5
+    b = Batch(8, 2, D, [n], [0], seed=79, spread=0)
+    pages = b.pages.copy()
+    g = np.random.default_rng(80)
+    parts = {0: (0, 0), 22: (16, 6), 24: (24, 0), 26: (24, 2), 28: (24, 4)}   # values at the scale 4
+    for t in range(n):
+        key = np.zeros(D)
+        key[:2] = parts[pattern[t // step % len(pattern)]]
+        for h in range(2):
+            value = g.choice([2.0 ** power, 2.0 ** power, 2.0 ** (power - 1), -2.0 ** (power - 2)], D)
+            value[::3] = 2.0 ** power
+            F.store(pages[b.bt[0, t // BS], h], D, t % BS, key, value)
+    b.host(pages)
+    k, v = b.rows(0)
+    assert np.array_equal(k[:, 0].sum(-1), np.array([pattern[t // step % len(pattern)] for t in range(n)]))
+    assert np.abs(v).max() == 2.0 ** power
+    return b, n
+
+
+LN2 = float(np.log(2.0))
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("pattern", [(0, 26, 26), (0, 24, 24, 26), (0, 24, 24), (0, 22, 22, 22), (0, 22), (28, 0, 28)])
+def test_decode_values_of_2_to_96_behind_a_base_that_stays(D, splits, pattern):
+    """Values up to 2^96 stay in range however far scores have risen above the first chunk's: sums in which every
+    key counts up to 2^26 times the base's are within the rule by which the base moves, or move it. The largest
+    sum of weights, over all lanes and waves, times 2^96 has to stay below 2^128. (A wave's chunks are the pattern.)"""
+    b, n = _large_values(D, pattern, 32, 4 * splits)
+    q = torch.ones(1, 8, D, dtype=torch.bfloat16)
+    out = cw.decode_attn_fp4(q.cuda(), b.cache, torch.from_numpy(b.bt).cuda(), torch.tensor([n], dtype=torch.int32).cuda(),
+                             LN2, num_splits=splits)
+    _check_attention(_f64(out), _f64(q), *b.rows(0), n - 1, LN2, f"D={D} {pattern}")
+
+
+@pytest.mark.parametrize("splits", [0, 3])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("pattern", [(0, 24, 24), (0, 24, 24, 26), (28, 0, 28)])
+def test_prefill_values_of_2_to_96_behind_a_base_that_stays(D, splits, pattern):
+    b, n = _large_values(D, pattern, 64, 4)
+    b.P, b.S, b.T, b.cu = [n - 6], [6], 6, np.array([0, 6], np.int32)
+    q = torch.ones(6, 8, D, dtype=torch.bfloat16)
+    out = _run_prefill(b.meta(), q.cuda(), b.cache, LN2, splits)
+    _check_attention(out, _f64(q), *b.rows(0), n - 6, LN2, f"D={D} {pattern}")
+
+
 @pytest.mark.parametrize("splits", [1, 3])
 def test_decode_lengths_out_of_range_and_foreign_blocks(splits):
     """A length beyond the table counts as the table's; a negative one as 0; blocks outside the pool are zero keys
