@@ -11,6 +11,7 @@ TEST INFRASTRUCTURE ONLY (see the package docstring).
 from __future__ import annotations
 
 import math
+from fractions import Fraction
 
 import numpy as np
 
@@ -152,3 +153,32 @@ def rotate(x, cos_sin, interleaved: bool):
         c, s = cos_sin[:, None, j, 0], cos_sin[:, None, j, 1]
         x[:, :, a], x[:, :, b] = x[:, :, a] * c - x[:, :, b] * s, x[:, :, b] * c + x[:, :, a] * s
     return x
+
+
+def exact_rotation(row, cos_sin, interleaved: bool):
+    """One row [D] rotated by cos_sin [n, 2] in rational arithmetic: a list of D Fractions (finite inputs). Two
+    products may lie further apart than the 53 bits of a double."""
+    out = [Fraction(float(u)) for u in row]
+    n = len(cos_sin)
+    for j in range(n):
+        a, b = (2 * j, 2 * j + 1) if interleaved else (j, j + n)
+        (x, y), (c, s) = (out[a], out[b]), (Fraction(float(t)) for t in cos_sin[j])
+        out[a], out[b] = x * c - y * s, y * c + x * s
+    return out
+
+
+def exact_codes(row):
+    """(codes [D], scale bytes [D / 32]) of a row of Fractions, as `round_rows` has them of 64-bit values; the
+    code of a negative value that rounds to zero, or of zero, is 0."""
+    codes, scales = [], []
+    for at in range(0, len(row), GROUP):
+        group = row[at:at + GROUP]
+        e = MIN_EXP
+        while e < MAX_EXP and max(map(abs, group)) > 7 * Fraction(2) ** e:
+            e += 1
+        scales.append(e + 127)
+        for u in group:
+            a = abs(u) / Fraction(2) ** e
+            c = min(range(8), key=lambda i: (abs(a - Fraction(VALUES[i])), i % 2))
+            codes.append(c + 8 if u < 0 and c else c)
+    return np.array(codes, np.uint8), np.array(scales, np.uint8)

@@ -106,7 +106,7 @@ __device__ __forceinline__ Unit find_unit(const int32_t* cu, const int32_t* plen
 // A value next to a border of two codes has to fall on its side of it, so keys are rotated by the
 // difference of two products without cancellation error (t = w s; d = x c - t; d - (w s - t), at
 // most 1.5 units off in the last place), and a wave that holds a value within 4 such units of a
-// border (they all have a mantissa of 2 bits) rotates again in 64 bits: few waves do.
+// border (they all have a mantissa of 2 bits) rotates again, exactly: few waves do.
 // HBM-bound: reads 2 (Hq + 2 Hkv) D bytes a row, writes 2 Hq D + 17/16 Hkv D. 16,128 rows of 32 / 8 heads of 128:
 // 72 us, 4.8 TB/s (a copy 4.8 to 5.3); 64 requests of one row 4.7 us in a captured graph, 18 called one by one
 // with a split of the projection's rows and the read, which is the host's time. A wave with 16 tokens of a head at a
@@ -144,21 +144,28 @@ __device__ __forceinline__ float turned(float x, float w, float c, float s) {
   return fmaf(x, c, -t) - fmaf(w, s, -t);
 }
 // The same with its last bit set where it is not exact: rounded on to fewer bits it goes where the
-// exact value goes, as it is never halfway by rounding alone.
+// exact value goes, as it is never halfway by rounding alone. Both products are exact in 64 bits, their sum is not
+// where they lie more than 53 bits apart (a tiny partner beside a border): what the sum lost decides where the rest of
+// its 53 bits is zero, and is less than that rest otherwise. (Few waves look at it: computed for all values it took 9
+// registers more, a wave a SIMD, and 16,128 rows 2 % more time; so, with six waves a SIMD named, none.)
 __device__ __forceinline__ float turned_to_odd(float x, float w, float c, float s) {
   asm volatile("" : "+v"(c), "+v"(s));   // (else the table is converted ahead of the loop over heads, in 32 registers)
-  const double y = fma(double(x), double(c), -(double(w) * double(s)));
+  const double a = double(x) * double(c), b = -(double(w) * double(s)), y = a + b;
   const float v = float(y);
-  const double rest = y - double(v);
-  const uint32_t b = __float_as_uint(v);
-  if (rest == 0. || (b & 1) != 0 || !(fabsf(v) > 0x1p-110f) || !(fabsf(v) < INFINITY)) return v;   // (a code of so small a value is zero)
-  return __uint_as_float((rest > 0.) == (v > 0.f) ? b + 1 : b - 1);
+  double rest = y - double(v);
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(rest == 0.) != 0, 0)) {
+    const double lost = fabs(a) >= fabs(b) ? b - (y - a) : a - (y - b);   // a + b - y
+    if (rest == 0.) rest = lost;
+  }
+  const uint32_t bits = __float_as_uint(v);
+  if (rest == 0. || (bits & 1) != 0 || !(fabsf(v) > 0x1p-110f) || !(fabsf(v) < INFINITY)) return v;   // (a code of so small a value is zero)
+  return __uint_as_float((rest > 0.) == (v > 0.f) ? bits + 1 : bits - 1);
 }
 
 // HALVES: column j is paired with j + pairs; else 2 j with 2 j + 1. ONCE: rows in and queries out pass the caches'
 // order of use.
 template <int D, bool HALVES, bool ONCE>
-__global__ __launch_bounds__(kThreads) void rope_append_fp4_kernel(const AppendArgs a) {
+__global__ __launch_bounds__(kThreads, 6) void rope_append_fp4_kernel(const AppendArgs a) {
   constexpr int PC = D / 16;    // columns a lane holds
   constexpr int NT = HALVES ? PC : PC / 2;   // (cos, sin) pairs a lane needs
   using Words = typename Piece<D>::Bf16;     // PC bfloat16 values

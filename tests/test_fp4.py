@@ -2,6 +2,7 @@
 import copy
 import ctypes
 import pickle
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -119,6 +120,41 @@ def test_rotate_is_the_projections_rotation_and_multiplication_of_complex_number
     z = (x[..., :32:2] + 1j * x[..., 1:32:2]) * np.exp(1j * ang[:, :16])[:, None]
     assert np.allclose(part[..., :32:2], z.real) and np.allclose(part[..., 1:32:2], z.imag)
     assert np.array_equal(part[..., 32:], x[..., 32:])
+
+
+@pytest.mark.parametrize("s,codes,scale", [
+    # 1.25 + d, -(2.5 - d) and 7 - d of d = 2^-60: 1.5, -2, and 6 at scale 1
+    (-2.0 ** -20, [3, 12, 7], 127),
+    # 1.25 - d, -(2.5 + d) and 7 + d, which needs the scale 2: halves just below 0.625, above 1.25, above 3.5
+    (2.0 ** -20, [1, 11, 6], 128),
+    # the ties themselves go to the even code
+    (0.0, [2, 12, 7], 127),
+])
+def test_exact_codes_of_hand_worked(s, codes, scale):
+    """Borders of codes and of a scale with a product beside them that lies below the 53 bits of a double."""
+    tiny = 2.0 ** -40
+    row = np.zeros(32)
+    row[:6] = [1.25, tiny, -2.5, tiny, 7.0, -tiny]
+    cos_sin = np.stack([np.ones(3), np.full(3, s)], -1)
+    turned = F.exact_rotation(row, cos_sin, True)
+    assert turned[0] == Fraction(5, 4) - Fraction(tiny) * Fraction(s) and turned[1] == Fraction(tiny) + Fraction(5, 4) * Fraction(s)
+    assert F.rotate(row[None, None], cos_sin[None], True)[0, 0, 0] == 1.25   # (what 64 bits make of it)
+    got, scales = F.exact_codes(turned)
+    assert got[:6:2].tolist() == codes and scales.tolist() == [scale]
+
+
+def test_exact_codes_are_those_of_64_bits_where_these_hold_the_values():
+    g = np.random.default_rng(5)
+    x = g.choice([0.0, 0.25, 0.75, -1.25, 2.5, 5.0, 7.0, 3.3, -0.1], (6, 1, 64)) * 2.0 ** g.integers(-4, 5, (6, 1, 1))
+    ang = np.stack([g.choice([0.5, 1.0], (6, 16)), g.choice([0.0, -0.25, 2.0 ** -12], (6, 16))], -1)
+    for interleaved in (False, True):
+        turned = F.rotate(x, ang, interleaved)
+        want, scales = F.round_rows(turned)
+        for i in range(6):
+            exact = F.exact_rotation(x[i, 0], ang[i], interleaved)
+            assert [float(u) for u in exact] == turned[i, 0].tolist()
+            got, e = F.exact_codes(exact)
+            assert np.array_equal(got, np.where(want[i, 0] == 8, 0, want[i, 0])) and np.array_equal(e, scales[i, 0])
 
 
 # ---------------------------------------------------------------- refusals

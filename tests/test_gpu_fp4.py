@@ -3,8 +3,8 @@ attention over the values a cache stands for, oracle.attention).
 
 Bounds, derived from the roundings (eps/2 of bf16 is 2^-8):
 
-* append: pages are compared byte by byte with the oracle's, which rounds the rotation in 64 bits:
-  the call's codes are those of exact arithmetic. q is an output rounding, 2^-8 |q|, plus the
+* append: pages are compared byte by byte with the oracle's, which rounds the rotation in 64 bits
+  (or, beside borders that these do not resolve, in rational arithmetic): the call's codes are those of exact arithmetic. q is an output rounding, 2^-8 |q|, plus the
   rotation's: 2^-24 of a product and of the sum, taken as 2^-22 of the products' magnitudes.
 * rows: exact.
 * attention: with A = sum p|v| / sum p, the probabilities' rounding to bf16 before the product
@@ -174,6 +174,55 @@ def test_append_values_beside_borders(D, interleaved):
     cw.rope_append_fp4(b.meta(), k, v, b.cache, rope=rope, interleaved=interleaved)
     torch.cuda.synchronize()
     _check_append(b, None, k, v, rope, interleaved, None, "borders")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("size", [0, -96, 100])
+def test_append_values_beside_borders_below_64_bits(D, interleaved, size):
+    """Keys next to a border of two codes, or of two scales, by as little as 2^-230 of it: a double holds 2^-53. The
+    codes are those of rational arithmetic. (`size`: the keys' power of two.)"""
+    n, T = D // 2, 10
+    b = Batch(1, 1, D, [3], [T], seed=68, held=[3])
+    _, _, v = _append_inputs(b)
+    borders = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, -1.25, -2.5, -5.0, 0.75])
+    near = borders[torch.randint(0, 12, (T, 1, n), generator=b.g)]
+    near[:, :, ::16] = torch.where(torch.rand(T, 1, n // 16, generator=b.g) < 0.5, 6.0, 7.0)
+    far = torch.exp2(-torch.randint(20, 126 + min(size, 0), (T, 1, n), generator=b.g).float())   # (times 2^size a bf16 value)
+    far = far * torch.randint(-1, 2, (T, 1, n), generator=b.g)
+    first = torch.rand(T, 1, n, generator=b.g) < 0.5   # the column of a pair that is beside a border
+    cols = [torch.where(first, near, far), torch.where(first, far, near)]
+    k = (torch.stack(cols, -1).flatten(2) if interleaved else torch.cat(cols, -1)) * 2.0 ** size
+    k = k.to(torch.bfloat16).cuda()
+    rope = torch.ones(T + 3, n, 2)
+    rope[:, :, 1] = torch.exp2(-torch.randint(20, 105, (T + 3, n), generator=b.g).float()) * \
+        (2 * torch.randint(0, 2, (T + 3, n), generator=b.g) - 1)
+    cw.rope_append_fp4(b.meta(), k, v, b.cache, rope=rope.cuda(), interleaved=interleaved)
+    torch.cuda.synchronize()
+    pages = b.cache.pages.cpu().numpy()
+    for t in range(T):
+        exact = F.exact_rotation(_f64(k)[t, 0], _f64(rope)[t + 3], interleaved)
+        codes, scales = F.exact_codes(exact)
+        got, at = (x[(t + 3) % BS] for x in F.unpack(pages[b.bt[0, (t + 3) // BS], 0], D)[0])
+        got = np.where(got == 8, 0, got)   # (minus zero is zero)
+        assert np.array_equal(at, scales), (t, at, scales)
+        off = np.flatnonzero(got != codes)
+        assert not len(off), f"token {t}: {len(off)} of {D}, column {off[0]} is {got[off[0]]}, should be {codes[off[0]]}"
+
+
+def test_append_products_that_leave_fp32():
+    """A table of more than 1 (scaled angles): both products of a pair leave fp32, their difference does not, their sum does."""
+    b = Batch(2, 2, 128, [0], [20], seed=69, held=[0])
+    _, k, v = _append_inputs(b)
+    k.copy_(((torch.rand(k.shape, generator=b.g) * 0.02 + 0.97) * 3.3e38).to(torch.bfloat16))
+    rope = torch.tensor([1.2, 1.3]).expand(20, 64, 2).contiguous()
+    rope[10:] = torch.tensor([1.3, -1.2])   # (the other column of a pair)
+    rope = rope.cuda()
+    cw.rope_append_fp4(b.meta(), k, v, b.cache, rope=rope)
+    torch.cuda.synchronize()
+    turned = F.rotate(_f64(k), _f64(rope), False)
+    assert (np.abs(turned[:10, :, :64]) < 2.0 ** 127).all() and (np.abs(turned[:10, :, 64:]) > 2.0 ** 128).all()
+    _check_append(b, None, k, v, rope, False, None, "beyond fp32")
 
 
 def test_append_cancelling_rotations():
