@@ -48,10 +48,13 @@ HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra"]
 # branches only; structurizing them makes the register allocator keep two
 # copies of the 64-register output accumulator across the branch arms, which
 # overflows the 256-register budget of two waves per SIMD. The calls of the
-# 8-bit path and over the 4-bit cache promise where NaN codes, scales and values go, so comparisons with NaN have
-# to mean what they say there (the product's code is the same either way, the
-# prefill takes the same time). Runs of keys are joined by cw_kernels.hip, which
-# only multiplies and adds their values: a NaN log-sum-exp does not get there.
+# 8-bit path and over the 4-bit cache promise where NaN codes, scales and values
+# go, so comparisons with NaN have to mean what they say there (the product's
+# code is the same either way, the prefill takes the same time). Runs of keys
+# are joined in two places. cw_fp8.hip joins those of both decode calls, whose
+# log-sum-exps may be NaN, and the 4-bit prefill's where they are many.
+# cw_kernels.hip merges the others, and only multiplies and adds their values:
+# the prefill kernels write a large number in place of a NaN log-sum-exp.
 EXTRA_FLAGS = {"cw_kernels.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"],
                "cw_fp8_prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true", "-fhonor-nans"],
                "cw_fp8_linear.hip": ["-fhonor-nans"],

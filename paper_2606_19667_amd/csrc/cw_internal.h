@@ -101,8 +101,9 @@ cw_status check_cache_fp8(const char* what, const void* k8, const void* v8, cons
 cw_status check_cache_fp4(const char* what, const void* pages, const int32_t* block_table, int32_t num_kv_heads,
                           int32_t head_dim, int32_t block_size, int32_t num_blocks);
 
-// Launches the join of a decode attention's runs (`what`: the call's name): part_o fp32 [parts, rows, head_dim],
-// part_lse fp32 [parts, rows], out bf16 [rows, head_dim]; parts <= kMaxSplits, head_dim 64 or 128.
+// Launches the join of the runs of a decode attention, or of a prefill of few rows in many runs (`what`: the call's
+// name): part_o fp32 [parts, rows, head_dim], part_lse fp32 [parts, rows] (-inf: a run that adds nothing; a NaN makes
+// its row NaN), out bf16 [rows, head_dim]; parts <= kMaxSplits, head_dim 64 or 128, rows below 2^24.
 cw_status decode_join(const char* what, int32_t head_dim, const float* part_o, const float* part_lse, int32_t parts,
                       int64_t rows, void* out, void* stream);
 

@@ -347,6 +347,21 @@ def test_4_bit_sources_are_built_with_nan_honoured():
         assert honor[-1] == "-fhonor-nans", s
 
 
+def test_the_join_of_runs_is_built_with_nan_honoured():
+    """The decode's runs, and the prefill's where they are many, are joined by a kernel of another source: a NaN
+    log-sum-exp has to make its row NaN there too."""
+    import os
+    from paper_2606_19667_amd import build
+    homes = []
+    for s in build.HIP_SOURCES:
+        with open(os.path.join(build.CSRC, s)) as fh:
+            if "cw_status cw::decode_join(" in fh.read():
+                homes.append(s)
+    assert len(homes) == 1
+    honor = [f for f in build.HIP_FLAGS + build.EXTRA_FLAGS.get(homes[0], []) if f.endswith("honor-nans")]
+    assert honor[-1] == "-fhonor-nans", homes
+
+
 @pytest.mark.parametrize("again", [copy.copy, copy.deepcopy, lambda m: pickle.loads(pickle.dumps(m))], ids=["copy", "deepcopy", "pickle"])
 def test_copies_of_a_used_batch_hand_over_their_own_arrays(again):
     """What a call keeps of a batch's host arrays goes into the library as their address: a copy of the batch, or one
