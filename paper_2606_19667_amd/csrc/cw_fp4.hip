@@ -884,8 +884,9 @@ extern "C" cw_status cw_decode_attn_fp4(const void* q, const void* pages, const 
   const int64_t grid = int64_t(batch) * num_kv_heads * head_tiles * num_splits;
   if (grid > kMaxGrid) return cw::fail(CW_EUNSUPPORTED, w + ": batch too large");
   auto* const s = static_cast<hipStream_t>(stream);
-  // A cache that the last-level cache (256 MiB) cannot hold is read past it. us, 64 requests of about 10,367 tokens,
-  // 720 MB: 138 against 153; 8 heads of 9,000 tokens, 10 MB, read again and again: 60 against 55.
+  // What the last-level cache (256 MiB) cannot hold is read past it. us, 64 requests of about 10,367 tokens,
+  // 720 MB: 138 against 153; 8 heads of 9,000 tokens, 10 MB, read again and again: 60 against 55. The host knows the
+  // table's width alone: short sequences behind a table for long ones are read past the cache, too.
   const bool once = int64_t(batch) * bt_stride * num_kv_heads * 17 * head_dim > (int64_t(256) << 20);
   auto* const kernel = head_dim == 128 ? (once ? decode_attn_fp4_kernel<128, true> : decode_attn_fp4_kernel<128, false>)
                                        : (once ? decode_attn_fp4_kernel<64, true> : decode_attn_fp4_kernel<64, false>);

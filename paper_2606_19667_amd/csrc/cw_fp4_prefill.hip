@@ -101,10 +101,11 @@ struct Geom {
 // is written in products(x - 2), 2 x - 3 and 2 x - 2, and first read (K) in 2 x - 1; the stage that it
 // replaces (step x - 3) was last read in 2 x - 4.
 //
-// 8 requests of 2,112 rows behind 3,136 keys, 32 / 8 heads of 128: 960 to 1,005 us by card, 1.2 PFLOP/s, what a large library
-// product of bf16 reaches on the same card (1.18): the matrix pipe is busy 58 % of the cycles at 2.0 GHz, and a fourth
+// 8 requests of 2,112 rows behind 3,136 keys, 32 / 8 heads of 128: 960 to 1,005 us by card, 1.15 to 1.21 PFLOP/s, where a
+// library product of 8,192^3 in bf16 reaches 1.18 to 1.40: the matrix pipe is busy 58 % of the cycles at 2.0 GHz, and a fourth
 // less matrix work takes 13 % off, 32 multiply-adds less of the softmax nothing. A step of lightly loaded units is 1.2 to
-// 1.4 us. 6 x ~411 rows behind ~700 keys, 28 / 4 heads, 42 us: the longest entry's 24 steps, behind a start in which
+// 1.4 us. 6 x ~411 rows behind ~700 keys, 28 / 4 heads, 42 to 46 us by card (one card: 41.5 in a loop and 42.2 in a captured
+// graph on the same data, 44.1 and 43.2 on three inputs in turn): the longest entry's 24 steps, behind a start in which
 // every workgroup reads its queries and three steps' pages (29 MB).
 //
 // SPLIT: the entries are runs of a tile's keys (a plan of several runs), and each writes its part, zeros and
@@ -317,9 +318,10 @@ void suffix_prefill_fp4_kernel(const PrefillArgs a) {
   constexpr int RA = 4;   // operands in flight ahead of their MFMA
   constexpr int NPV = kBlocks * DT, NQK = 2 * KS, N = NPV + NQK;
   // The loaded codes are converted beside the last products and the next loads go out beside the last of these: the
-  // later, the more time a load has. us with both from the first QK product on, 6 operands ahead / so: 8 x 2,112 rows
-  // behind 3,136 keys 988 / 976, 6 x ~411 behind ~700 47.6 / 46.5, 1 x 2,000 54.8 / 53.5; twice the conversions beside
-  // each of half as many products 980, 46.9, 53.5; a further step of loads in flight, copied into place 991, 47.4, 54.9.
+  // later, the more time a load has. us (of each pair on one card) with both from the first QK product on, 6 operands
+  // ahead / so: 8 x 2,112 rows behind 3,136 keys 988 / 976, 6 x ~411 behind ~700 47.6 / 46.5, 1 x 2,000 54.8 / 53.5;
+  // twice the conversions beside each of half as many products 980, 46.9, 53.5; a further step of loads in flight,
+  // copied into place 991, 47.4, 54.9.
   constexpr int WIDEN_AT = N - G::UNITS;
   bf16x8 op[RA];
   int st0 = 0, st1 = G::STAGE, st2 = 2 * G::STAGE;   // LDS places of the current step and the two after it

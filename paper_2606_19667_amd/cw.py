@@ -1180,8 +1180,8 @@ def rope_append_fp4(meta: BatchMeta, k: torch.Tensor, v: torch.Tensor, cache: Fp
 def cache_rows_fp4(meta: BatchMeta, cache: Fp4KvCache, k_rows: torch.Tensor | None = None,
                    v_rows: torch.Tensor | None = None, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
     """cw_cache_rows_fp4: the keys and values of the suffix rows of `meta` as the
-    4-bit cache holds them, (k_rows, v_rows) bf16 [total_s, Hkv, D]. (A prefix is
-    the suffix of a description whose prefix lengths are zero.)"""
+    4-bit cache holds them, (k_rows, v_rows) bf16 [total_s, Hkv, D], both of them. (A
+    prefix is the suffix of a description whose prefix lengths are zero.)"""
     if DEBUG_CHECK_COPIES:
         meta.check_device_copies()
     hkv, D = meta.num_kv_heads, meta.head_dim
@@ -1276,7 +1276,9 @@ def suffix_prefill_attn_split_fp4(meta: BatchMeta, q: torch.Tensor, cache: Fp4Kv
 
 
 def decode_split_count_fp4(batch: int, num_q_heads: int, num_kv_heads: int, max_len: int) -> int:
-    """A split count for cw_decode_attn_fp4 with sequences of up to max_len tokens. Joining
+    """A split count for cw_decode_attn_fp4 with sequences of up to max_len tokens (of about that
+    many: where most are far shorter, as behind a table of the longest that may come, their runs are
+    mostly empty ones, whose zeros are written and joined all the same). Joining
     runs is a second launch, 2 us: none below 640 tokens. Above, two workgroups per compute
     unit with runs of 192 tokens at least, and with many tiles (requests x KV heads) runs of about
     2,000 tokens, which even out ragged lengths. Measured in captured graphs, us (32 / 8 heads of 128): 1 x
@@ -1301,10 +1303,13 @@ def decode_attn_fp4(q: torch.Tensor, cache: Fp4KvCache, block_table: torch.Tenso
                     out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """cw_decode_attn_fp4: one query row per request, q [batch, Hq, D] bf16, over
     the first seq_lens [batch] (int32, device) tokens of its row of block_table
-    [batch, stride] (int32, device); returns out [batch, Hq, D] bf16. `workspace`
-    (uint8, device) is allocated when not given; calls that may run at the same
-    time, captured ones among them, need one each. What a call of this section
-    allocates belongs to its stream."""
+    [batch, stride] (int32, device); returns out [batch, Hq, D] bf16. The lengths
+    stay on the device: num_splits, and the size of the workspace with it, are by
+    default decode_split_count_fp4's of the table's 16 * stride tokens, so a caller
+    whose table is far wider than its sequences passes the count of their length.
+    `workspace` (uint8, device) is allocated when not given; calls that may run at
+    the same time, captured ones among them, need one each. What a call of this
+    section allocates belongs to its stream."""
     if q.dim() != 3:
         raise ValueError(f"q must be [batch, Hq, D], got {tuple(q.shape)}")
     B, hq, D = q.shape
