@@ -147,7 +147,8 @@ __device__ __forceinline__ float turned(float x, float w, float c, float s) {
 // exact value goes, as it is never halfway by rounding alone. Both products are exact in 64 bits, their sum is not
 // where they lie more than 53 bits apart (a tiny partner beside a border): what the sum lost decides where the rest of
 // its 53 bits is zero, and is less than that rest otherwise. (Few waves look at it: computed for all values it took 9
-// registers more, a wave a SIMD, and 16,128 rows 2 % more time; so, with six waves a SIMD named, none.)
+// registers more, a wave a SIMD, and 16,128 rows 2 % more time; so, with six waves a SIMD named, none. Not marked
+// as the unlikely way it spills 110 registers.)
 __device__ __forceinline__ float turned_to_odd(float x, float w, float c, float s) {
   asm volatile("" : "+v"(c), "+v"(s));   // (else the table is converted ahead of the loop over heads, in 32 registers)
   const double a = double(x) * double(c), b = -(double(w) * double(s)), y = a + b;
